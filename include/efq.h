@@ -293,6 +293,105 @@ efq_status_t efq_calibrate(const void* q, const void* k, const void* v, const fl
                            const float* taus, int n_tau, const float* hs, int n_h, double* sums, double* rho,
                            float* best_tau, float* best_h, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * Serving beside the forwards: rotary positions, a paged cache of keys and values, and softmax attention over it.  (The
+ * paper has no counterpart; these are the steps of a model around its attention.)  Elements are bf16 or fp16, d = 128.
+ * Their rows need 16-byte aligned pointers and strides of multiples of 8 elements, channels contiguous (ALIGNMENT
+ * otherwise).  Descriptors are host structs that are read during the call only.
+ * ------------------------------------------------------------------------------------------------------------------ */
+typedef enum { EFQ_BF16 = 0, EFQ_FP16 = 1 } efq_dtype_t;
+
+/* Rotary positions with one to four axes (a text's running index; time, height and width of a video).  The first
+ * R = pairs[0] + ... + pairs[n_axes - 1] pairs of channels are turned, the channels behind them are left as they are.
+ * Pair p belongs to the axis whose run of pairs holds it; its angle is the token's position on that axis times inv_freq[p],
+ * formed in double and reduced to one turn there, so positions may lie far out:
+ *   (y0, y1) = (x0 cos a - x1 sin a, x0 sin a + x1 cos a), in FP32, rounded once.
+ *   inv_freq     double [R], device: radians per position
+ *   pairs        R a multiple of 8 and at most d / 2 (UNSUPPORTED otherwise)
+ *   interleaved  0: pair p is channels (p, p + R); 1: channels (2p, 2p + 1) */
+typedef struct {
+    const double* inv_freq;
+    int32_t n_axes;
+    int32_t pairs[4];
+    int32_t interleaved;
+} efq_rotary_t;
+
+/* Rows of one tensor of `heads` heads, read from src and written to dst, with the strides of batch entries, heads and
+ * tokens in elements.  dst may be src with the same strides; any other overlap of the two is not allowed. */
+typedef struct {
+    const void* src;
+    void* dst;
+    int32_t heads;
+    int64_t src_batch, src_head, src_token;
+    int64_t dst_batch, dst_head, dst_token;
+} efq_rows_t;
+
+/* Turns q and k (either may be NULL) of B batch entries of S tokens in one launch.  What a projection leaves token-major can
+ * be written as the forwards read it, [B, H, S, d].
+ *   positions  int32, device: token t of entry b has position positions[a * position_axis + b * position_batch + t] on axis a
+ *   inverse    nonzero: turned back.  A rotation's gradient: the gradient of src is the gradient of dst turned back.
+ * B == 0 or S == 0 is a valid no-op.  Errors: INVALID_ARG (null pointers, sizes below zero, no axis or more than four), UNSUPPORTED,
+ * ALIGNMENT, ARCH, CUDA. */
+efq_status_t efq_rotary(const efq_rows_t* q, const efq_rows_t* k, const int32_t* positions, int64_t position_axis, int64_t position_batch,
+                        int B, int64_t S, int d, int dtype, const efq_rotary_t* rotary, int inverse, void* stream);
+
+/* A paged cache and the sequences of a step.  Key and value i of sequence s lie on page page_table[s * table_stride + i / page_size],
+ * at token i % page_size.  The step's new tokens lie one sequence after the other in [total, ...] tensors: sequence s owns the
+ * tokens cu_seqlens[s] to cu_seqlens[s + 1] - 1, which are the last of its seq_lens[s] tokens.  The three tables are DEVICE memory, so that a
+ * recorded graph follows them from replay to replay.
+ *   k, v         [n_pages, n_heads, page_size, 128], strides in elements (a token-major cache is one with other strides)
+ *   page_size    a power of two from 16 to 4096
+ *   max_pages    entries of a row of page_table; those behind a sequence's last page are not read */
+typedef struct {
+    void *k, *v;
+    int64_t k_page, k_head, k_token;
+    int64_t v_page, v_head, v_token;
+    int32_t n_pages, n_heads, page_size;
+    const int32_t* page_table;
+    int64_t table_stride;
+    int32_t max_pages;
+    const int32_t* cu_seqlens;   /* [n_seqs + 1], from 0, not decreasing */
+    const int32_t* seq_lens;     /* [n_seqs], the new tokens among them */
+    int32_t n_seqs;
+} efq_paged_t;
+
+/* Writes the new keys and values of a step into the cache, the keys rotated on the way, and rotates the queries beside
+ * them in the same launch.
+ *   k, v       [total, n_heads, d], strides of token and head (the batch strides are not read); dst and its strides are not read
+ *   q          NULL, or the queries [total, heads, d]
+ *   rotary     NULL: nothing is turned (keys, values and queries are copied)
+ *   positions  int32 [axis][token] with position_axis between axes; NULL: a token's index in its sequence, on every axis
+ * Tokens behind cu_seqlens[n_seqs] are left alone, in q too.  A token whose index is below zero or past max_pages * page_size,
+ * or whose entry in the page table is not a page (a padding token's -1), is not stored; its q is rotated all the same.  Two
+ * tokens must not share a place: pages that sequences have in common are full.  Errors as for efq_rotary. */
+efq_status_t efq_paged_append(const efq_rows_t* k, const efq_rows_t* v, const efq_rows_t* q, int64_t total, const int32_t* positions,
+                              int64_t position_axis, const efq_paged_t* cache, int d, int dtype, const efq_rotary_t* rotary, void* stream);
+
+/* Softmax attention of a step's new tokens over the paged cache, no low-bit operand anywhere: for token i of a sequence of n new
+ * and len tokens, o = sum_j p_j v_j / sum_j p_j with p_j = exp(scale q k_j - max) over the keys j < len, with `causal` j <= i + len - n.
+ * One token (a decode step) to long chunks of a prompt, and batches of both.
+ *   q       src: queries [total, heads, d] with strides of token and head; dst: o, of the same type, with its own strides.  heads is
+ *           a multiple of cache->n_heads, at most 128 times as many; query head h reads KV head h / (heads / n_heads)
+ *   lse     NULL, or float [total, heads]: log sum_j exp(scale q k_j); what two partial contexts are joined by
+ *   max_seqlen_q  the most new tokens that any sequence has: chooses the kernel.  Sequences with more are computed all the same.
+ *   softmax_scale  <= 0 selects 1/sqrt(d)
+ *   workspace  device, 256-byte aligned, >= efq_paged_attention_workspace_bytes(...); its contents need not be kept and need no
+ *           preparation.  Calls that may overlap (other streams, graphs that run beside one another) need one each.
+ * Scores, maxima, sums and the output's accumulator are FP32, the probabilities of a tile are rounded to the elements' type for the product
+ * with V.  A token that sees no key gets a row of zeros and lse = -inf.  Rows behind cu_seqlens[n_seqs] are left alone.  What lies in the pages
+ * behind a sequence's last token does not matter; an infinity or NaN in a value of the sequence makes NaN of its channel in
+ * every row of the 128 x 128 tiles that hold it.  Rows are NaN where the page table names no page (an entry below
+ * zero or from n_pages on, a sequence longer than max_pages * page_size), and in blocks in which a bounded device-side wait expired.
+ * Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, WORKSPACE, ARCH, CUDA.  total == 0 or n_seqs == 0 is a valid no-op. */
+size_t efq_paged_attention_workspace_bytes(int Hq, int Hkv, int max_seqlen_q, int d);
+efq_status_t efq_paged_attention_fwd(const efq_rows_t* q, float* lse, int64_t total, int max_seqlen_q, const efq_paged_t* cache, int d,
+                                     int dtype, int causal, float softmax_scale, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Test hook as efq_attention_fwd_inject_timeout, for efq_paged_attention_fwd: K and V are not loaded.  The rows of `o` become NaN. */
+efq_status_t efq_paged_attention_fwd_inject_timeout(const efq_rows_t* q, float* lse, int64_t total, int max_seqlen_q, const efq_paged_t* cache,
+                                                    int d, int dtype, int causal, float softmax_scale, void* workspace,
+                                                    size_t workspace_bytes, void* stream);
+
 /* Synchronises `stream` and returns the device-side status word of the last forward that
  * used `workspace` (EFQ_OK, or EFQ_ERR_DEVICE_TIMEOUT if a bounded wait expired), or
  * EFQ_ERR_CUDA if the stream reports an error. */

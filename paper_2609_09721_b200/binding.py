@@ -26,7 +26,8 @@ EXPORTS = ["efq_probgen", "exp_then_quantize_probgen", "efq_attention_workspace_
            "efq_attention_fwd_host", "efq_attention_fwd_host_pipelined", "efq_attention_fwd_static", "efq_poll_status",
            "efq_attention_varlen_workspace_bytes", "efq_attention_fwd_varlen",
            "efq_exact_attention_fwd", "efq_relative_error", "efq_calibrate",
-           "efq_fp4_mma_peak_probe", "efq_stage_microbench", "efq_attention_fwd_inject_timeout",
+           "efq_rotary", "efq_paged_append", "efq_paged_attention_workspace_bytes", "efq_paged_attention_fwd",
+           "efq_paged_attention_fwd_inject_timeout", "efq_fp4_mma_peak_probe", "efq_stage_microbench", "efq_attention_fwd_inject_timeout",
            "efq_exact_attention_fwd_inject_timeout", "efq_status_string", "efq_version"]
 
 
@@ -38,6 +39,24 @@ class EfqParams(C.Structure):
 class EfqDebug(C.Structure):
     _fields_ = [("raw_scores", C.c_void_p), ("row_max", C.c_void_p), ("codes", C.c_void_p), ("scales", C.c_void_p),
                 ("batch", C.c_int32), ("head", C.c_int32), ("q_begin", C.c_int64), ("q_end", C.c_int64)]
+
+
+class EfqRotary(C.Structure):
+    _fields_ = [("inv_freq", C.c_void_p), ("n_axes", C.c_int32), ("pairs", C.c_int32 * 4), ("interleaved", C.c_int32)]
+
+
+class EfqRows(C.Structure):
+    _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("heads", C.c_int32),
+                ("src_batch", C.c_int64), ("src_head", C.c_int64), ("src_token", C.c_int64),
+                ("dst_batch", C.c_int64), ("dst_head", C.c_int64), ("dst_token", C.c_int64)]
+
+
+class EfqPaged(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_page", C.c_int64), ("k_head", C.c_int64), ("k_token", C.c_int64),
+                ("v_page", C.c_int64), ("v_head", C.c_int64), ("v_token", C.c_int64),
+                ("n_pages", C.c_int32), ("n_heads", C.c_int32), ("page_size", C.c_int32), ("page_table", C.c_void_p),
+                ("table_stride", C.c_int64), ("max_pages", C.c_int32), ("cu_seqlens", C.c_void_p), ("seq_lens", C.c_void_p),
+                ("n_seqs", C.c_int32)]
 
 
 class EfqError(RuntimeError):
@@ -104,6 +123,16 @@ def lib() -> C.CDLL:
         L.efq_calibrate.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i64, i64, i32, i32, f32,
                                     C.POINTER(C.c_float), i32, C.POINTER(C.c_float), i32, vp, C.POINTER(C.c_double),
                                     C.POINTER(C.c_float), C.POINTER(C.c_float), vp, C.c_size_t, vp]
+        rows, paged = C.POINTER(EfqRows), C.POINTER(EfqPaged)
+        L.efq_rotary.restype = i32
+        L.efq_rotary.argtypes = [rows, rows, vp, i64, i64, i32, i64, i32, i32, C.POINTER(EfqRotary), i32, vp]
+        L.efq_paged_append.restype = i32
+        L.efq_paged_append.argtypes = [rows, rows, rows, i64, vp, i64, paged, i32, i32, C.POINTER(EfqRotary), vp]
+        L.efq_paged_attention_workspace_bytes.restype = C.c_size_t
+        L.efq_paged_attention_workspace_bytes.argtypes = [i32, i32, i32, i32]
+        for f in (L.efq_paged_attention_fwd, L.efq_paged_attention_fwd_inject_timeout):
+            f.restype = i32
+            f.argtypes = [rows, vp, i64, i32, paged, i32, i32, i32, f32, vp, C.c_size_t, vp]
         L.efq_poll_status.restype = i32
         L.efq_poll_status.argtypes = [vp, vp]
         L.efq_fp4_mma_peak_probe.restype = i32
@@ -130,6 +159,7 @@ def _fastcall():
         efq_fastcall.set_functions(address(L.efq_attention_fwd), address(L.exp_then_quantize_attention_fwd),
                                    address(L.efq_probgen), address(L.exp_then_quantize_probgen),
                                    address(L.efq_attention_fwd_varlen), address(L.efq_attention_varlen_workspace_bytes))
+        efq_fastcall.set_paged_functions(address(L.efq_rotary), address(L.efq_paged_append), address(L.efq_paged_attention_fwd))
         _fast = efq_fastcall
     return _fast
 
@@ -419,6 +449,152 @@ def efq_calibrate(q, k, v, o_ref, taus, hs, causal: bool = False, softmax_scale:
     _check(st, "efq_calibrate")
     table = [[rho[i * n_h + j] for j in range(n_h)] for i in range(n_tau)]
     return table, (float(bt.value), float(bh.value))
+
+
+_ELEMENTS = {torch.bfloat16: 0, torch.float16: 1}
+
+
+class Rotary:
+    """Rotary positions with one to four axes, as efq_rotary and efq_paged_append take them: made once and kept.
+
+    inv_freq: float64 CUDA tensor [R], radians per position of each pair of channels; sections: pairs of each axis, in order, R in all (a
+    multiple of 8, at most 64); interleaved: pair p is channels (2p, 2p + 1) and not (p, p + R)."""
+
+    def __init__(self, inv_freq: torch.Tensor, sections, interleaved: bool = False):
+        sections = tuple(int(n) for n in sections)
+        assert inv_freq.is_cuda and inv_freq.dtype == torch.float64 and inv_freq.is_contiguous() and 1 <= len(sections) <= 4
+        assert min(sections) >= 0 and inv_freq.numel() == sum(sections)
+        self.inv_freq, self.sections = inv_freq, sections
+        self.c = EfqRotary(inv_freq.data_ptr(), len(sections), (C.c_int32 * 4)(*sections), int(bool(interleaved)))
+        self.address = C.addressof(self.c)
+
+    @classmethod
+    def of(cls, sections, theta: float = 10000.0, interleaved: bool = False, ladder_per_axis: bool = False, device=None):
+        """Frequencies theta^(-j/n): one ladder over all pairs (a text model, also with several axes), or one for each axis (video)."""
+        sections = tuple(int(n) for n in sections)
+        steps = [j / n for n in sections for j in range(n)] if ladder_per_axis else [j / sum(sections) for j in range(sum(sections))]
+        return cls(torch.tensor([float(theta) ** -x for x in steps], dtype=torch.float64, device=device or "cuda"), sections, interleaved)
+
+
+def _here(*tensors):
+    """The tensors are on the current device, whose streams the call uses."""
+    device = _raw_device()
+    for t in tensors:
+        assert t.get_device() == device, "tensors have to be on the current CUDA device"
+
+
+def _turned_out(x, out):
+    if out is None:
+        return torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    assert out.shape == x.shape and out.dtype is x.dtype and out.stride(-1) == 1
+    return out
+
+
+def efq_rotary(q, k, positions, rotary: Rotary, inverse: bool = False, q_out=None, k_out=None, stream=None):
+    """Rotary positions turned into q [B, Hq, S, 128] and k [B, Hkv, S, 128] (bf16 or fp16, any strides; either may be None) in one
+    launch.  positions: int32 [axes, S], or [axes, B, S].  q_out and k_out: the outputs (q and k themselves: in place); new tensors are
+    contiguous, as the forwards take them.  inverse: turned back, which is the gradient.  Returns (q_out, k_out)."""
+    x = q if q is not None else k
+    B, _, S, d = x.shape
+    assert d == 128 and positions.dtype is torch.int32 and positions.stride(-1) == 1 and positions.shape[0] == len(rotary.sections)
+    assert positions.shape[1:] in ((S,), (B, S))
+    _here(x, positions, rotary.inv_freq)
+    args = []
+    outs = []
+    for t, out in ((q, q_out), (k, k_out)):
+        if t is None:
+            args += (None, None, None, None, None)
+            outs.append(None)
+            continue
+        out = _turned_out(t, out)
+        assert t.shape[0] == B and t.shape[2] == S and t.shape[3] == d and t.dtype is x.dtype and (t.stride(3) == 1 or t.numel() == 0)
+        _here(t, out)
+        args += (t.data_ptr(), out.data_ptr(), t.shape, t.stride(), out.stride())
+        outs.append(out)
+    st = (_fast or _fastcall()).rotary(*args, positions.data_ptr(), positions.stride(0), positions.stride(1) if positions.dim() == 3 else 0, B, S,
+                                       _ELEMENTS[x.dtype], rotary.address, 1 if inverse else 0, _stream(stream))
+    if st:
+        _check(st, "efq_rotary")
+    return tuple(outs)
+
+
+def _cache_args(k_cache, v_cache, page_table, cu_seqlens, seq_lens, dtype):
+    """The cache [pages, Hkv, page_size, 128] and the step's int32 tables: page_table [n_seqs, max_pages], cu_seqlens [n_seqs + 1], seq_lens [n_seqs]."""
+    shape, table = k_cache.shape, page_table.shape
+    assert k_cache.dtype is dtype and v_cache.dtype is dtype and v_cache.shape == shape and len(shape) == 4 and shape[3] == 128
+    assert k_cache.stride(3) == 1 and v_cache.stride(3) == 1
+    i32 = torch.int32
+    assert page_table.dtype is i32 and cu_seqlens.dtype is i32 and seq_lens.dtype is i32
+    assert len(table) == 2 and page_table.stride(1) == 1 and cu_seqlens.shape == (table[0] + 1,) and seq_lens.shape == (table[0],)
+    assert cu_seqlens.is_contiguous() and seq_lens.is_contiguous()
+    _here(k_cache, v_cache, page_table, cu_seqlens, seq_lens)
+    return (k_cache.data_ptr(), v_cache.data_ptr(), shape, k_cache.stride(), v_cache.stride(), page_table.data_ptr(), table, page_table.stride(),
+            cu_seqlens.data_ptr(), seq_lens.data_ptr())
+
+
+def efq_paged_append(k, v, k_cache, v_cache, page_table, cu_seqlens, seq_lens, rotary: Optional[Rotary] = None, positions=None, q=None,
+                     q_out=None, stream=None):
+    """Writes the new keys (rotated) and values of a step, [total, Hkv, 128], into the paged cache [pages, Hkv, page_size, 128] and
+    rotates q [total, Hq, 128] beside them.  cu_seqlens, seq_lens, page_table: int32 CUDA tensors; seq_lens counts the new tokens too.
+    positions: int32 [axes, total], None: a token's index in its sequence.  Returns q_out, or None without q."""
+    total, Hkv, d = k.shape
+    dtype = k.dtype
+    assert v.shape == k.shape and v.dtype is dtype and d == 128 and Hkv == k_cache.shape[1]
+    assert (k.stride(2) == 1 and v.stride(2) == 1) or total == 0
+    _here(k, v)
+    cache = _cache_args(k_cache, v_cache, page_table, cu_seqlens, seq_lens, dtype)
+    if rotary is not None:
+        _here(rotary.inv_freq)
+    if positions is not None:
+        assert rotary is not None and positions.dtype is torch.int32 and positions.shape == (len(rotary.sections), total)
+        assert positions.stride(1) == 1 or total <= 1
+        _here(positions)
+    q_args = (None, None, None, None, None)
+    if q is not None:
+        assert q.dim() == 3 and q.shape[0] == total and q.shape[2] == d and q.dtype is dtype and (q.stride(2) == 1 or total == 0)
+        q_out = _turned_out(q, q_out)
+        _here(q, q_out)
+        q_args = (q.data_ptr(), q_out.data_ptr(), q.shape, q.stride(), q_out.stride())
+    ks, vs = k.stride(), v.stride()
+    st = (_fast or _fastcall()).paged_append(k.data_ptr(), None, k.shape, ks, ks, v.data_ptr(), None, v.shape, vs, vs, *q_args, total,
+                                             None if positions is None else positions.data_ptr(), 0 if positions is None else positions.stride(0),
+                                             *cache, _ELEMENTS[dtype], None if rotary is None else rotary.address, _stream(stream))
+    if st:
+        _check(st, "efq_paged_append")
+    return None if q is None else q_out
+
+
+def efq_paged_attention_workspace_bytes(Hq: int, Hkv: int, max_seqlen_q: int, d: int = 128) -> int:
+    return int(lib().efq_paged_attention_workspace_bytes(Hq, Hkv, max_seqlen_q, d))
+
+
+def _paged_attention_args(q, k_cache, v_cache, page_table, cu_seqlens, seq_lens, max_seqlen_q, o, lse, workspace):
+    total, Hq, d = q.shape
+    dtype = q.dtype
+    assert d == 128 and (q.stride(2) == 1 or total == 0)
+    o = _turned_out(q, o)
+    _here(q, o)
+    cache = _cache_args(k_cache, v_cache, page_table, cu_seqlens, seq_lens, dtype)
+    if lse is not None:
+        assert lse.dtype is torch.float32 and lse.shape == (total, Hq) and lse.is_contiguous()
+        _here(lse)
+    if workspace is None:
+        workspace = torch.empty(max(efq_paged_attention_workspace_bytes(Hq, k_cache.shape[1], max_seqlen_q, d), 256), dtype=torch.uint8, device=q.device)
+    _here(workspace)
+    return total, o, cache, workspace
+
+
+def efq_paged_attention_fwd(q, k_cache, v_cache, page_table, cu_seqlens, seq_lens, max_seqlen_q: int, causal: bool = True,
+                            softmax_scale: float = 0.0, o=None, lse=None, workspace=None, stream=None):
+    """Softmax attention of a step's new tokens q [total, Hq, 128] over a paged cache [pages, Hkv, page_size, 128] (tables as for
+    efq_paged_append); max_seqlen_q: the most new tokens of any sequence.  lse: optional fp32 [total, Hq] output.  Returns o, of q's type."""
+    total, o, cache, workspace = _paged_attention_args(q, k_cache, v_cache, page_table, cu_seqlens, seq_lens, max_seqlen_q, o, lse, workspace)
+    st = (_fast or _fastcall()).paged_attention(q.data_ptr(), o.data_ptr(), q.shape, q.stride(), o.stride(), None if lse is None else lse.data_ptr(), total,
+                                                max_seqlen_q, *cache, _ELEMENTS[q.dtype], 1 if causal else 0, softmax_scale, workspace.data_ptr(),
+                                                workspace.numel(), _stream(stream))
+    if st:
+        _check(st, "efq_paged_attention_fwd")
+    return o
 
 
 def efq_poll_status(workspace, stream=None) -> int:

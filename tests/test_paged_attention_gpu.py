@@ -1,0 +1,185 @@
+"""efq_paged_attention_fwd against softmax attention in 64 bits: query rows of a KV group from one to many, lengths around the tiles and
+pages, every type and layout, steps of many sequences, and what must not matter (stale pages, unused entries, other rows)."""
+import math
+
+import pytest
+import torch
+
+from paged_reference import D, Paged
+from paper_2609_09721_b200 import binding
+
+pytestmark = pytest.mark.gpu
+
+
+def _run(p, causal=True, lse=True, scale=0.0, **more):
+    o = torch.full((p.total, p.Hq, D), 7.0, dtype=p.dtype, device="cuda")
+    l = torch.full((p.total, p.Hq), 7.0, device="cuda") if lse else None
+    got = binding.efq_paged_attention_fwd(p.d_q, p.d_k_cache, p.d_v_cache, *p.tables, more.pop("max_q", p.max_q), causal, scale, o, l, **more)
+    assert got is o
+    return o, l
+
+
+def _check(p, o, lse, causal=True, scale=None):
+    want, want_lse, tol, lse_tol = p.attention(causal, scale)
+    n = int(p.cu[-1])
+    assert torch.isfinite(o[:n]).all()
+    off = (o[:n].double() - want[:n]).abs() - tol[:n]
+    assert float(off.max() if off.numel() else 0.0) <= 0.0, float(off.max())
+    assert (o[n:] == 7.0).all()                                   # rows behind the last sequence
+    if lse is not None:
+        seen = torch.isfinite(want_lse[:n])
+        assert (lse[:n][~seen] == -math.inf).all()
+        off = ((lse[:n].double() - want_lse[:n]).abs() - lse_tol[:n])[seen]
+        assert float(off.max() if off.numel() else 0.0) <= 0.0, float(off.max())
+        assert (lse[n:] == 7.0).all()
+
+
+# (lens, Hq, Hkv, page): rows of a KV group are Hq / Hkv times the new tokens
+FEW = [
+    ([(1, 1)], 1, 1, 16), ([(1, 2)], 8, 8, 16), ([(1, 63)], 4, 1, 16), ([(1, 64)], 8, 2, 32), ([(1, 65)], 8, 2, 64), ([(1, 128)], 4, 4, 128),
+    ([(1, 8191)], 32, 8, 16), ([(1, 20001)], 1, 1, 64), ([(1, 300)], 16, 1, 16), ([(1, 1000)], 5, 1, 256), ([(1, 999)], 3, 1, 16),
+    ([(1, 777)], 17, 1, 32), ([(1, 500)], 32, 1, 16), ([(1, 5)], 24, 2, 1024),
+    ([(4, 4)], 4, 1, 16), ([(2, 130)], 8, 1, 16), ([(5, 2000)], 32, 8, 32), ([(8, 1025)], 8, 2, 16), ([(16, 40)], 1, 1, 16),
+    ([(3, 64)], 20, 4, 64), ([(32, 4000)], 2, 2, 128), ([(7, 7)], 4, 1, 16), ([(9, 700)], 3, 1, 16),
+    ([(1, n) for n in (1, 70, 300, 4096, 16, 129, 2000)], 32, 8, 16), ([(1, 1 + 37 * i) for i in range(130)], 8, 2, 16),
+    ([(1 + i % 4, 4 + 53 * i) for i in range(40)], 8, 4, 32), ([(1, 17)] * 700, 2, 2, 16), ([(0, 50), (1, 60), (0, 0), (2, 2), (0, 9)], 4, 2, 16),
+]
+CHUNK = [
+    ([(33, 33)], 1, 1, 16), ([(128, 128)], 1, 1, 16), ([(129, 129)], 2, 2, 16), ([(256, 257)], 1, 1, 128), ([(300, 300)], 4, 1, 64),
+    ([(300, 9000)], 32, 8, 64), ([(64, 5000)], 4, 4, 32), ([(17, 1200)], 2, 1, 16), ([(100, 3001)], 28, 4, 16), ([(77, 800)], 10, 2, 256),
+    ([(50, 51)], 3, 1, 16),
+    ([(2000, 2100)], 2, 2, 128), ([(1, 700), (300, 400), (5, 2000), (0, 10), (128, 128), (1, 1), (40, 999)], 8, 2, 16),
+    ([(37, 37 + 100 * i) for i in range(20)], 4, 2, 64), ([(1024, 1024)], 4, 4, 512),
+]
+
+
+@pytest.mark.parametrize("lens,Hq,Hkv,page", FEW + CHUNK)
+@pytest.mark.parametrize("causal", [True, False])
+def test_against_64_bits(lens, Hq, Hkv, page, causal):
+    p = Paged(lens, Hq, Hkv, page, seed=len(lens) + Hq)
+    _check(p, *_run(p, causal), causal)
+
+
+@pytest.mark.parametrize("lens,Hq,Hkv,page", [FEW[6], FEW[16], FEW[24], CHUNK[5], CHUNK[12]])
+def test_fp16(lens, Hq, Hkv, page):
+    p = Paged(lens, Hq, Hkv, page, torch.float16, seed=3)
+    _check(p, *_run(p))
+    o, _ = _run(p, lse=False)
+    _check(p, o, None)
+
+
+@pytest.mark.parametrize("max_q", [1, 6, 40, 4000])
+def test_the_announced_length_only_chooses_the_kernel(max_q):
+    """Sequences with more new tokens than announced are computed all the same."""
+    p = Paged([(70, 200), (1, 900), (33, 33)], 8, 2, 16, seed=5)
+    o, lse = _run(p, max_q=max_q)
+    _check(p, o, lse)
+
+
+@pytest.mark.parametrize("lens,Hq,Hkv", [([(1, 900), (2, 77)], 8, 2), ([(200, 900), (3, 500)], 8, 2)])
+def test_strides(lens, Hq, Hkv):
+    """q as a part of a wider projection, o into a wider buffer, a token-major cache, a table that is a part of a wider one, rows behind the
+    last sequence: they are left as they were."""
+    p = Paged(lens, Hq, Hkv, 32, seed=6, token_major=True, tail=5)
+    want = _run(p)
+    _check(p, *want)
+    wide = torch.zeros(p.total, Hq + 3, D + 64, dtype=p.dtype, device="cuda")
+    wide[:, 1:Hq + 1, 64:] = p.d_q
+    out = torch.full((p.total, 2 * Hq, D), 7.0, dtype=p.dtype, device="cuda")
+    table = torch.full((len(lens), p.d_table.shape[1] + 9), 1 << 30, dtype=torch.int32, device="cuda")
+    table[:, :-9] = p.d_table
+    binding.efq_paged_attention_fwd(wide[:, 1:Hq + 1, 64:], p.d_k_cache, p.d_v_cache, table, p.d_cu, p.d_seq_lens, p.max_q, o=out[:, ::2])
+    assert torch.equal(out[:, ::2], want[0]) and (out[:, 1::2] == 7.0).all()
+
+
+@pytest.mark.parametrize("lens,Hq", [([(8, 3), (1, 0), (2, 500)], 2), ([(300, 100), (64, 0), (5, 5)], 2), ([(40, 1)], 32)])
+def test_tokens_that_see_nothing(lens, Hq):
+    """More new tokens than tokens: the first ones see no key and get zeros, with lse = -inf."""
+    p = Paged([(a, b) for a, b in lens], Hq, 2, 16, seed=7)
+    o, lse = _run(p)
+    _check(p, o, lse)
+    a, b = lens[0]
+    assert (o[:a - b] == 0).all() and (lse[:a - b] == -math.inf).all()
+
+
+@pytest.mark.parametrize("lens,Hq,Hkv", [([(1, 700), (2, 90)], 4, 2), ([(90, 700), (2, 90)], 8, 2)])
+def test_pages_that_are_none(lens, Hq, Hkv):
+    """An entry that names no page, or a sequence longer than its row of the table: rows of NaN, for that sequence alone."""
+    p = Paged(lens, Hq, Hkv, 16, seed=8)
+    want, _ = _run(p)
+    n = lens[0][0]
+    for bad in (-1, -2**31, p.d_k_cache.shape[0], 2**31 - 1):
+        table = p.d_table.clone()
+        table[0, 0] = bad
+        o = binding.efq_paged_attention_fwd(p.d_q, p.d_k_cache, p.d_v_cache, table, p.d_cu, p.d_seq_lens, p.max_q)
+        assert torch.isnan(o[:n]).all() and torch.equal(o[n:], want[n:]), bad
+    for length in (p.d_table.shape[1] * 16 + 1, 2**31 - 1):
+        lens_now = p.d_seq_lens.clone()
+        lens_now[0] = length
+        o = binding.efq_paged_attention_fwd(p.d_q, p.d_k_cache, p.d_v_cache, p.d_table, p.d_cu, lens_now, p.max_q)
+        assert torch.isnan(o[:n]).all() and torch.equal(o[n:], want[n:])
+    lens_now = p.d_seq_lens.clone()
+    lens_now[0] = -5                                             # no keys
+    o = binding.efq_paged_attention_fwd(p.d_q, p.d_k_cache, p.d_v_cache, p.d_table, p.d_cu, lens_now, p.max_q)
+    assert (o[:n] == 0).all() and torch.equal(o[n:], want[n:])
+
+
+@pytest.mark.parametrize("lens,Hq,Hkv", [([(1, 3000)], 8, 2), ([(200, 3000)], 8, 2), ([(1, 10 + i) for i in range(50)], 8, 2)])
+def test_the_same_call_gives_the_same_bits(lens, Hq, Hkv):
+    p = Paged(lens, Hq, Hkv, 16, seed=9)
+    first = _run(p)
+    workspace = torch.full((binding.efq_paged_attention_workspace_bytes(Hq, Hkv, p.max_q),), 255, dtype=torch.uint8, device="cuda")
+    for _ in range(3):
+        again = _run(p, workspace=workspace)
+        assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
+@pytest.mark.parametrize("n", [1, 100])
+def test_large_scores_and_scales(n):
+    """Scores far from zero: the running maximum keeps the exponentials in range, in whatever order the keys come."""
+    p = Paged([(n, 1500)], 4, 2, 64, seed=10, hot=0)
+    k = p.k[0].double()
+    k[:, :, 0] = torch.linspace(-200, 200, 1500)[:, None]        # grows along the keys: every tile has a new maximum
+    p.k[0] = k.to(p.dtype)
+    at, slot = torch.arange(1500) // 64, torch.arange(1500) % 64
+    p.d_k_cache[p.table[0].long()[at].cuda(), :, slot.cuda()] = p.k[0].cuda()
+    p.d_q[..., 0] = 3.0
+    for scale in (0.0, 0.5, 1e-3):
+        _check(p, *_run(p, scale=scale), scale=scale or None)
+
+
+def test_recorded_into_a_graph_it_follows_the_tables():
+    """Lengths, tables and the cache live on the device: a replay computes what they say then."""
+    p = Paged([(1, 400), (1, 900), (1, 31)], 8, 2, 16, seed=11)
+    o = torch.zeros(p.total, 8, D, dtype=p.dtype, device="cuda")
+    workspace = torch.empty(binding.efq_paged_attention_workspace_bytes(8, 2, 1), dtype=torch.uint8, device="cuda")
+    lens, table = p.d_seq_lens.clone(), p.d_table.clone()
+    call = lambda: binding.efq_paged_attention_fwd(p.d_q, p.d_k_cache, p.d_v_cache, table, p.d_cu, lens, 1, o=o, workspace=workspace)  # noqa: E731
+    call()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for cut in (0, 17, 30):
+        lens.copy_(p.d_seq_lens - cut)
+        o.zero_()
+        graph.replay()
+        q = Paged([(1, m - cut) for _, m in p.lens], 8, 2, 16, seed=11)
+        for i, (_, m) in enumerate(q.lens):
+            q.k[i], q.v[i] = p.k[i][:m], p.v[i][:m]
+        q.d_q = p.d_q
+        _check(q, o, None)
+
+
+def test_on_a_side_stream():
+    p = Paged([(1, 3000), (60, 500)], 8, 2, 16, seed=12)
+    want, _ = _run(p)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    o = torch.zeros_like(want)
+    o.record_stream(s)
+    workspace = torch.empty(binding.efq_paged_attention_workspace_bytes(8, 2, 60), dtype=torch.uint8, device="cuda")
+    s.wait_stream(torch.cuda.current_stream())
+    for _ in range(5):
+        binding.efq_paged_attention_fwd(p.d_q, p.d_k_cache, p.d_v_cache, *p.tables, 60, o=o, workspace=workspace, stream=s)
+    s.synchronize()
+    assert torch.equal(o, want)

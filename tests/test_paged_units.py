@@ -1,0 +1,116 @@
+"""How the kernels of the paged attention share a step's work (csrc/paged_units.h), on the host: the sums in closed form, and that
+the runs of all CTAs hold every unit once, in order, with the CTA that begins a query tile named rightly."""
+import ctypes
+import random
+import subprocess
+
+import pytest
+
+from paper_2609_09721_b200 import build
+
+HARNESS = r"""
+#include "paged_units.h"
+struct Reader {
+    const int32_t *cu, *lens;
+    int step, keys, causal;
+    efq::SeqWork operator()(int s, int& begin) const { begin = cu[s]; return {cu[s + 1] - cu[s], lens[s], step, keys, causal, 0}; }
+};
+extern "C" int64_t before(int lq, int len, int step, int keys, int causal, int n) { return efq::SeqWork{lq, len, step, keys, causal, 0}.units_before(n); }
+extern "C" int tile_of(int lq, int len, int step, int keys, int causal, int64_t off) { return efq::SeqWork{lq, len, step, keys, causal, 0}.tile_of(off); }
+// segments of all CTAs: (cta, begins, seq, head, token0, tokens, base, j0, j1, n) each; the number of them, -1 if there are more than fit
+extern "C" int64_t segments(const int32_t* cu, const int32_t* lens, int n_seqs, int heads, int step, int keys, int causal, int grid, int32_t* out, int64_t most)
+{
+    const Reader read{cu, lens, step, keys, causal};
+    int64_t total = 0, n = 0;
+    int b;
+    for (int s = 0; s < n_seqs; ++s) total += read(s, b).units_per_head() * heads;
+    const int64_t ctas = grid < total ? grid : total;
+    for (int64_t c = 0; c < ctas; ++c) {
+        efq::PagedRun run{};
+        int64_t off = efq::paged_first_unit(total, ctas, c);
+        for (int s = 0; s < n_seqs; ++s) {
+            const efq::SeqWork w = read(s, b);
+            if (off < w.units_per_head() * heads) { efq::paged_begin_run(w, s, off, total, ctas, c, &run); break; }
+            off -= w.units_per_head() * heads;
+        }
+        efq::PagedWalk<Reader> walk(read, n_seqs, heads, run);
+        efq::PagedSegment g;
+        for (bool first = true; walk.next(g); first = false) {
+            if (n == most) return -1;
+            const int32_t v[10] = {(int32_t)c, first ? run.begins : (int32_t)c, g.seq, g.head, g.token0, g.tokens, g.base, g.j0, g.j1, g.n};
+            for (int i = 0; i < 10; ++i) out[10 * n + i] = v[i];
+            ++n;
+        }
+    }
+    return n;
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def lib(tmp_path_factory):
+    d = tmp_path_factory.mktemp("units")
+    (d / "units.cpp").write_text(HARNESS)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-I", build.CSRC, str(d / "units.cpp"), "-o", str(d / "units.so")], check=True)
+    so = ctypes.CDLL(str(d / "units.so"))
+    so.before.restype = so.segments.restype = ctypes.c_int64
+    so.tile_of.argtypes = [ctypes.c_int] * 5 + [ctypes.c_int64]
+    so.segments.argtypes = [ctypes.POINTER(ctypes.c_int32)] * 2 + [ctypes.c_int] * 6 + [ctypes.POINTER(ctypes.c_int32), ctypes.c_int64]
+    return so
+
+
+def _units(lq, len_, step, keys, causal):
+    """Units of each query tile, one by one."""
+    out = []
+    for first in range(0, lq, step):
+        seen = max(0, len_ - lq + min(first + step, lq)) if causal else len_
+        out.append(max(1, -(-seen // keys)))
+    return out
+
+
+def test_units_in_closed_form(lib):
+    rng = random.Random(1)
+    for _ in range(4000):
+        lq, len_ = rng.choice([1, rng.randint(1, 40), rng.randint(1, 700)]), rng.choice([0, 1, rng.randint(0, 900), rng.randint(0, 9000)])
+        step, keys, causal = rng.choice([1, 2, 3, 4, 8, 18, 36, 42, 64, 256]), rng.choice([64, 128]), rng.randint(0, 1)
+        want = _units(lq, len_, step, keys, causal)
+        n = rng.randint(0, len(want))
+        assert lib.before(lq, len_, step, keys, causal, n) == sum(want[:n]), (lq, len_, step, keys, causal, n)
+        tile = rng.randrange(len(want))
+        off = sum(want[:tile]) + rng.randrange(want[tile])
+        assert lib.tile_of(lq, len_, step, keys, causal, off) == tile
+
+
+def test_units_of_the_longest_sequences(lib):
+    """A whole prompt of two million tokens: the sum stays exact in 64 bits."""
+    lq = len_ = 2_000_003
+    assert lib.before(lq, len_, 64, 128, 1, -(-lq // 64)) == sum(_units(lq, len_, 64, 128, 1))
+    assert lib.before(1, 2**31 - 1, 16, 64, 1, 1) == 2**25
+
+
+@pytest.mark.parametrize("seed", range(60))
+def test_runs_hold_every_unit_once(lib, seed):
+    rng = random.Random(seed)
+    n, heads, grid = rng.choice([1, 2, 5, 40, 300]), rng.choice([1, 2, 8]), rng.choice([1, 3, 148])
+    step, keys, causal = rng.choice([1, 4, 5, 16, 64, 84]), rng.choice([64, 128]), rng.randint(0, 1)
+    lens_q = [rng.choice([0, 1, 1, rng.randint(1, 9), rng.randint(1, 300)]) for _ in range(n)]
+    lens_k = [rng.choice([0, 1, rng.randint(1, 200), rng.randint(1, 4000)]) for _ in range(n)]
+    cu = [sum(lens_q[:i]) for i in range(n + 1)]
+    want = [(s, h, cu[s] + t * step, j, u) for s in range(n) for h in range(heads)
+            for t, u in enumerate(_units(lens_q[s], lens_k[s], step, keys, causal)) for j in range(u)]
+    most = len(want) + 1
+    out = (ctypes.c_int32 * (10 * most))()
+    got = lib.segments((ctypes.c_int32 * (n + 1))(*cu), (ctypes.c_int32 * n)(*lens_k), n, heads, step, keys, causal, grid, out, most)
+    assert got >= 0
+    rows = [tuple(out[10 * i:10 * i + 10]) for i in range(got)]
+    assert [(s, h, t0, j, u) for _, _, s, h, t0, _, _, j0, j1, u in rows for j in range(j0, j1)] == want
+    sizes, begun = {}, {}
+    for c, begins, s, h, t0, tokens, base, j0, j1, u in rows:
+        sizes[c] = sizes.get(c, 0) + j1 - j0
+        if j0 == 0:
+            begun[s, h, t0] = c
+        assert begun[s, h, t0] == begins                       # also the second and later CTAs of a query tile
+        first = t0 - cu[s]
+        assert tokens == min(step, lens_q[s] - first) and base == lens_k[s] - lens_q[s] + first
+    if want:
+        assert sorted(sizes) == list(range(min(grid, len(want)))) and max(sizes.values()) - min(sizes.values()) <= 1

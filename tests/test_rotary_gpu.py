@@ -1,0 +1,215 @@
+"""efq_rotary and efq_paged_append against their formulas in 64 bits: axes, pair layouts, partly turned channels, far positions, types,
+strides, and what has to stay as it was."""
+import math
+
+import pytest
+import torch
+
+from paged_reference import D, Paged, rotate, rotate_slack
+from paper_2609_09721_b200 import binding
+
+pytestmark = pytest.mark.gpu
+
+CASES = [                                    # sections, interleaved, one ladder an axis, first position
+    ((64,), False, False, 0), ((64,), True, False, 7), ((22, 21, 21), True, True, 0), ((16, 24, 24), False, False, 900000),
+    ((20, 12), False, True, -40), ((8, 8, 8), True, False, 1 << 30), ((8,), False, False, 3), ((0, 64), False, False, 5),
+    ((10, 20, 30, 4), False, True, 2**31 - 400), ((5, 3), True, False, 11),
+]
+
+
+def _rotary(sections, interleaved, per_axis, theta=1e6):
+    return binding.Rotary.of(sections, theta, interleaved, per_axis)
+
+
+def _positions(axes, tokens, first):
+    t = torch.arange(tokens, dtype=torch.int32, device="cuda")
+    return torch.stack([(t // (a + 1) + first).int() for a in range(axes)])
+
+
+def _near(got, want, slack, what=""):
+    u = torch.finfo(got.dtype).eps / 2
+    tiny = 2.0 ** -25 if got.dtype == torch.float16 else 0.0
+    off = (got.double() - want).abs() - (u * want.abs() * (1 + 2.0 ** -10) + slack + tiny)
+    assert float(off.max()) <= 0.0, (what, float(off.max()))
+
+
+@pytest.mark.parametrize("sections,interleaved,per_axis,first", CASES)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("inverse", [False, True])
+def test_against_64_bits(sections, interleaved, per_axis, first, dtype, inverse):
+    g = torch.Generator(device="cuda").manual_seed(1)
+    for B, S, Hq, Hkv in ((1, 1, 1, 1), (2, 37, 5, 3), (1, 301, 8, 2)):
+        q, k = (torch.randn(B, H, S, D, generator=g, device="cuda").to(dtype) for H in (Hq, Hkv))
+        r, pos = _rotary(sections, interleaved, per_axis), _positions(len(sections), S, first)
+        got = binding.efq_rotary(q, k, pos, r, inverse)
+        for x, y in zip((q, k), got):
+            assert y.is_contiguous()
+            _near(y, rotate(x, pos, r.inv_freq, sections, interleaved, inverse), rotate_slack(x, dtype, sections, interleaved))
+            R = sum(sections)
+            assert torch.equal(y[..., 2 * R:], x[..., 2 * R:])       # what lies behind the turned channels
+
+
+@pytest.mark.parametrize("B,S,Hq,Hkv", [(1, 1, 40, 8), (3, 130, 28, 4), (1, 5000, 3, 1), (65, 1, 2, 2), (1, 4097, 24, 24)])
+def test_layouts_in_place_and_one_tensor(B, S, Hq, Hkv):
+    """Token-major views of a projection in, head-major out; in place; q or k alone: the same bits."""
+    g = torch.Generator(device="cuda").manual_seed(2)
+    sections = (22, 21, 21)
+    r = _rotary(sections, True, True)
+    pos = _positions(3, S, 4)
+    qkv = torch.randn(B, S, Hq + 2 * Hkv, D, generator=g, device="cuda").bfloat16()
+    kept = qkv.clone()
+    q, k = qkv[:, :, :Hq].transpose(1, 2), qkv[:, :, Hq:Hq + Hkv].transpose(1, 2)
+    yq, yk = binding.efq_rotary(q, k, pos, r)
+    assert torch.equal(qkv, kept)
+    dense = binding.efq_rotary(q.contiguous(), k.contiguous(), pos, r)
+    assert torch.equal(yq, dense[0]) and torch.equal(yk, dense[1])
+    alone, none = binding.efq_rotary(q, None, pos, r)
+    assert none is None and torch.equal(alone, yq)
+    none, alone = binding.efq_rotary(None, k, pos, r)
+    assert none is None and torch.equal(alone, yk)
+    batched = torch.stack([pos + b for b in range(B)], dim=1)
+    per_entry, _ = binding.efq_rotary(q, None, batched, r)
+    for b in range(B):
+        assert torch.equal(per_entry[b:b + 1], binding.efq_rotary(q[b:b + 1], None, pos + b, r)[0])
+    binding.efq_rotary(q, k, pos, r, q_out=q, k_out=k)
+    assert torch.equal(qkv[:, :, :Hq].transpose(1, 2), yq) and torch.equal(qkv[:, :, Hq:Hq + Hkv].transpose(1, 2), yk)
+    assert torch.equal(qkv[:, :, Hq + Hkv:], kept[:, :, Hq + Hkv:])
+
+
+def test_the_inverse_is_the_gradient():
+    """d <w, rotate(x)> / dx is w turned back: against differences of the formula, and against the formula's own derivative."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    sections = (20, 12)
+    r, pos = _rotary(sections, False, False), _positions(2, 9, 100)
+    x = torch.randn(1, 2, 9, D, generator=g, device="cuda", dtype=torch.float64).requires_grad_()
+    w = torch.randn(1, 2, 9, D, generator=g, device="cuda").bfloat16()
+    y = rotate(x.detach(), pos, r.inv_freq, sections, False)
+    step = 2.0 ** -10
+    got, _ = binding.efq_rotary(w, None, pos, r, inverse=True)
+    for at in [(0, 0, 0, 0), (0, 1, 8, 31), (0, 1, 5, 32), (0, 0, 3, 63), (0, 0, 3, 64), (0, 1, 2, 127)]:
+        e = torch.zeros_like(x.detach())
+        e[at] = step
+        by_difference = ((rotate(x.detach() + e, pos, r.inv_freq, sections, False) - y) * w.double()).sum() / step
+        # the formula is linear: the difference is exact but for the rounding of y (2^-53 of a sum of 2304 values, over the step)
+        assert abs(float(got[at]) - float(by_difference)) <= abs(float(by_difference)) * 2.0 ** -8 + 2.0 ** -20, at
+    rotated = []
+    R = 32
+    axis = [a for a, n in enumerate(sections) for _ in range(n)]
+    angle = torch.stack([pos[axis[p]].double() * r.inv_freq[p] for p in range(R)], dim=-1)
+    a, b = x[..., :R], x[..., R:2 * R]
+    rotated = torch.cat((a * angle.cos() - b * angle.sin(), a * angle.sin() + b * angle.cos(), x[..., 2 * R:]), dim=-1)
+    grad, = torch.autograd.grad((rotated * w.double()).sum(), x)
+    _near(got, grad, rotate_slack(w, torch.bfloat16, sections, False))
+
+
+@pytest.mark.parametrize("lens,Hq,Hkv,page", [
+    ([(1, 1)], 1, 1, 16), ([(1, 64)], 8, 2, 64), ([(1, 1 + 31 * i) for i in range(70)], 32, 8, 16), ([(300, 300)], 4, 4, 16),
+    ([(129, 1000)], 5, 1, 128), ([(0, 9), (3, 40), (0, 0), (17, 17), (0, 5), (1, 4096)], 8, 2, 32), ([(1, 20)] * 2000, 2, 1, 16),
+    ([(2500, 5000)], 28, 4, 256),
+])
+@pytest.mark.parametrize("own_positions", [False, True])
+def test_append(lens, Hq, Hkv, page, own_positions):
+    """New tokens of every sequence land in their places, keys rotated; nothing else in the cache changes, nor do rows behind the last one."""
+    tail = 3
+    sections = (16, 24, 24) if own_positions else (64,)
+    p = Paged(lens, Hq, Hkv, page, seed=4, tail=tail, token_major=len(lens) > 2)
+    r = _rotary(sections, own_positions, False)
+    n = int(p.cu[-1])
+    g = torch.Generator(device="cuda").manual_seed(5)
+    k, v = (torch.randn(p.total, Hkv, D, generator=g, device="cuda").bfloat16() for _ in range(2))
+    index = torch.cat([torch.arange(m - a, m) for a, m in lens] + [torch.zeros(tail, dtype=torch.long)]).cuda()
+    pos = torch.stack([index // 100, index // 10 % 10, index % 10]).int() if own_positions else index[None].int()
+    want_k, want_v = p.d_k_cache.clone(), p.d_v_cache.clone()
+    place = [(int(p.table[s, i // page]), i % page) for s, (a, m) in enumerate(lens) for i in range(m - a, m)]
+    pages, slots = (torch.tensor([x[j] for x in place], device="cuda") for j in (0, 1))
+    turned = lambda x: rotate(x.transpose(0, 1), pos, r.inv_freq, sections, own_positions).transpose(0, 1)  # noqa: E731
+    q_out = torch.full((p.total, Hq, D), 7.0, dtype=p.dtype, device="cuda")
+    got = binding.efq_paged_append(k, v, p.d_k_cache, p.d_v_cache, *p.tables, r, pos if own_positions else None, p.d_q, q_out)
+    assert got is q_out and (q_out[n:] == 7.0).all()
+    _near(q_out[:n], turned(p.d_q)[:n], rotate_slack(p.d_q, p.dtype, sections, own_positions)[:n])
+    _near(p.d_k_cache[pages, :, slots], turned(k)[:n], rotate_slack(k, p.dtype, sections, own_positions)[:n])
+    want_k[pages, :, slots] = p.d_k_cache[pages, :, slots]
+    want_v[pages, :, slots] = v[:n]
+    same = lambda a, b: torch.equal(a.contiguous().view(torch.int16), b.contiguous().view(torch.int16))  # noqa: E731
+    assert same(p.d_k_cache, want_k) and same(p.d_v_cache, want_v)
+
+
+def test_append_without_rotation_and_without_queries():
+    p = Paged([(5, 50), (1, 300)], 4, 2, 16, seed=6)
+    k, v = (torch.randn(6, 2, D, device="cuda").bfloat16() for _ in range(2))
+    assert binding.efq_paged_append(k, v, p.d_k_cache, p.d_v_cache, *p.tables) is None
+    for t, (s, i) in enumerate([(0, 45), (0, 46), (0, 47), (0, 48), (0, 49), (1, 299)]):
+        at = (int(p.table[s, i // 16]), slice(None), i % 16)
+        assert torch.equal(p.d_k_cache[at], k[t]) and torch.equal(p.d_v_cache[at], v[t])
+
+
+def test_tokens_without_a_place_are_not_stored():
+    """A padding token's entry -1, an entry past the cache, an index below zero or past the table: nothing is written for them."""
+    p = Paged([(2, 40), (3, 30), (4, 2), (1, 100)], 4, 2, 16, seed=7)
+    table = p.d_table.clone()
+    table[0, 2] = -1                              # tokens 38 and 39 of sequence 0
+    table[1, 1] = p.d_k_cache.shape[0]            # tokens 27 to 29 of sequence 1
+    lens = p.d_seq_lens.clone()
+    lens[3] = p.d_table.shape[1] * 16 + 1         # the new token lies one past the table
+    k, v = (torch.randn(10, 2, D, device="cuda").bfloat16() for _ in range(2))
+    before_k, before_v = p.d_k_cache.clone(), p.d_v_cache.clone()
+    r = _rotary((64,), False, False)
+    q = binding.efq_paged_append(k, v, p.d_k_cache, p.d_v_cache, table, p.d_cu, lens, r, None, p.d_q)
+    assert torch.isfinite(q).all()
+    for t, i in ((7, 0), (8, 1)):                 # of sequence 2 the last two tokens have an index
+        at = (int(p.table[2, 0]), slice(None), i)
+        before_v[at] = v[t]
+        before_k[at] = p.d_k_cache[at]
+    assert torch.equal(before_v.view(torch.int16), p.d_v_cache.view(torch.int16)) and torch.equal(before_k.view(torch.int16), p.d_k_cache.view(torch.int16))
+
+
+def test_a_step_of_a_model():
+    """Appended keys and values are what the attention reads: a prompt in two chunks, then single tokens, against the whole in 64 bits."""
+    Hq, Hkv, page, sections = 8, 2, 16, (64,)
+    r = _rotary(sections, False, False)
+    g = torch.Generator(device="cuda").manual_seed(8)
+    total = 150
+    q, k, v = (torch.randn(total, H, D, generator=g, device="cuda").bfloat16() for H in (Hq, Hkv, Hkv))
+    k_cache, v_cache = (torch.full((12, Hkv, page, D), math.nan, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    table = torch.tensor([[7, 3, 11, 0, 5, 2, 9, 1, 10, 4, -1]], dtype=torch.int32, device="cuda")
+    o = torch.empty_like(q)
+    at = 0
+    for n in (100, 47, 1, 1, 1):
+        new = slice(at, at + n)
+        at += n
+        cu, lens = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([0, n], [at]))
+        turned = binding.efq_paged_append(k[new], v[new], k_cache, v_cache, table, cu, lens, r, None, q[new])
+        o[new] = binding.efq_paged_attention_fwd(turned, k_cache, v_cache, table, cu, lens, n)
+    pos = torch.arange(total, device="cuda", dtype=torch.int32)[None]
+    u = 2.0 ** -8
+    Q, K = (rotate(x.transpose(0, 1), pos, r.inv_freq, sections, False) for x in (q, k))      # [H, tokens, D]
+    seen = torch.ones(total, total, dtype=torch.bool, device="cuda").tril()
+    for h in range(Hq):
+        s = (Q[h] @ K[h // (Hq // Hkv)].T / math.sqrt(D))
+        # rotated q and k are rounded: u of each factor of every product, 2 u and u^2 of the sum of sizes
+        ds = (Q[h].abs() @ K[h // (Hq // Hkv)].abs().T / math.sqrt(D)).amax(1, keepdim=True) * (2.1 * u)
+        p = torch.softmax(s.masked_fill(~seen, -math.inf), dim=1)
+        V = v[:, h // (Hq // Hkv)].double()
+        tol = (torch.expm1(2 * ds) + 1.1 * u) * (p @ V.abs()) + u * (p @ V).abs()
+        assert float(((o[:, h].double() - p @ V).abs() - tol).max()) <= 0.0
+
+
+def test_recorded_into_a_graph():
+    p = Paged([(1, 30), (1, 200)], 4, 2, 16, seed=9)
+    r = _rotary((64,), False, False)
+    k, v = (torch.randn(2, 2, D, device="cuda").bfloat16() for _ in range(2))
+    q_out = torch.zeros_like(p.d_q)
+    call = lambda: binding.efq_paged_append(k, v, p.d_k_cache, p.d_v_cache, *p.tables, r, None, p.d_q, q_out)  # noqa: E731
+    call()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for back in (1, 14):                          # other lengths: other places and positions
+        p.d_seq_lens.copy_(p.seq_lens - back)
+        graph.replay()
+        want = torch.empty_like(q_out)
+        kc, vc = p.d_k_cache.clone(), p.d_v_cache.clone()
+        binding.efq_paged_append(k, v, kc, vc, *p.tables, r, None, p.d_q, want)
+        assert torch.equal(want, q_out) and torch.equal(vc.view(torch.int16), p.d_v_cache.view(torch.int16))
+        at = (int(p.table[1, (199 - back) // 16]), slice(None), (199 - back) % 16)
+        assert torch.equal(p.d_v_cache[at], v[1])
