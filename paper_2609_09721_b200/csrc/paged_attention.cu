@@ -1,10 +1,11 @@
 // efq_paged_attention_fwd: softmax attention of a step's new tokens over a paged cache.  paged_few.cuh holds the kernel for few query rows,
-// paged_walk.cuh how the work is shared; here are the kernel that joins parts and the entry points.
+// paged_chunk.cuh that for many, paged_units.h and paged_walk.cuh how the work is shared; here are the kernel that joins parts and the entry points.
 #include <cuda.h>
 
 #include <atomic>
 
 #include "efq_internal.cuh"
+#include "paged_chunk.cuh"
 #include "paged_few.cuh"
 
 namespace efq {
@@ -12,48 +13,56 @@ namespace {
 
 constexpr int kMaxCtas = 256;            // of the first kernel; the workspace has room for the parts of as many
 
-// Joins the parts of the query tiles that span CTAs.  blockIdx.x: the CTA that ended the tile, blockIdx.y: a row of it; four warps
-// take every fourth part each, a lane four channels.
-template <typename T, int kRows>
-__global__ void __launch_bounds__(128) paged_join_kernel(const __grid_constant__ PagedArgs A)
+// Joins the parts of the query tiles that span CTAs.  blockIdx.x: the CTA that ended the tile.  kWarps warps take a row, every kWarps-th
+// part each, a lane four channels.  Few rows may have a part from every CTA (one long context), many rows have two or three as a rule.
+// half_rows: rows of the first of the two halves of a tile of many rows (whole tokens); parts keep kRows / 2 for each half.
+template <typename T, int kRows, int kWarps>
+__global__ void __launch_bounds__(128) paged_join_kernel(const __grid_constant__ PagedArgs A, int half_rows)
 {
+    constexpr int kAtOnce = 4 / kWarps;         // rows of a block
     ptx::grid_wait();
-    const int c = blockIdx.x, r = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int c = blockIdx.x, lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) % kWarps, which = (threadIdx.x >> 5) / kWarps;
     const PagedRecord rec = {__ldcg(&A.records[c].first), __ldcg(&A.records[c].token0), __ldcg(&A.records[c].tokens), __ldcg(&A.records[c].head)};
-    if (rec.first < 0 || r >= rec.tokens * A.G) return;
-    auto slot = [&](int i) { return (2 * i + (i == rec.first ? 1 : 0)) * kRows + r; };
-    float top = -INFINITY;
-    for (int i = rec.first + lane; i <= c; i += 32) top = fmaxf(top, __ldcg(&A.part_ml[slot(i)].x));
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-    const float base = top == -INFINITY ? 0.0f : top;
-    float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    float l = 0.0f;
-#pragma unroll 4
-    for (int i = rec.first + warp; i <= c; i += 4) {
-        const float2 ml = __ldcg(&A.part_ml[slot(i)]);
-        const float4 y = __ldcg(reinterpret_cast<const float4*>(A.part_o + static_cast<int64_t>(slot(i)) * kPagedD) + lane);
-        const float f = paged_exp2(ml.x - base);
-        l = fmaf(ml.y, f, l);
-        x.x = fmaf(y.x, f, x.x); x.y = fmaf(y.y, f, x.y); x.z = fmaf(y.z, f, x.z); x.w = fmaf(y.w, f, x.w);
-    }
+    if (rec.first < 0) return;
     __shared__ float4 xs[4][32];
     __shared__ float ls[4];
-    xs[warp][lane] = x;
-    if (lane == 0) ls[warp] = l;
-    __syncthreads();
-    if (warp != 0) return;
+    for (int r = blockIdx.y * kAtOnce + which; r < rec.tokens * A.G; r += gridDim.y * kAtOnce) {
+        const int at = r < half_rows ? r : kRows / 2 + r - half_rows;
+        auto slot = [&](int i) { return (2 * i + (i == rec.first ? 1 : 0)) * kRows + at; };
+        float top = -INFINITY;
+        for (int i = rec.first + lane; i <= c; i += 32) top = fmaxf(top, __ldcg(&A.part_ml[slot(i)].x));
 #pragma unroll
-    for (int w = 1; w < 4; ++w) {
-        const float4 y = xs[w][lane];
-        x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
-        l += ls[w];
+        for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+        const float base = top == -INFINITY ? 0.0f : top;
+        float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        float l = 0.0f;
+#pragma unroll 4
+        for (int i = rec.first + warp; i <= c; i += kWarps) {
+            const float2 ml = __ldcg(&A.part_ml[slot(i)]);
+            const float4 y = __ldcg(reinterpret_cast<const float4*>(A.part_o + static_cast<int64_t>(slot(i)) * kPagedD) + lane);
+            const float f = paged_exp2(ml.x - base);
+            l = fmaf(ml.y, f, l);
+            x.x = fmaf(y.x, f, x.x); x.y = fmaf(y.y, f, x.y); x.z = fmaf(y.z, f, x.z); x.w = fmaf(y.w, f, x.w);
+        }
+        if (kWarps > 1) {
+            xs[warp][lane] = x;
+            if (lane == 0) ls[warp] = l;
+            __syncthreads();
+#pragma unroll
+            for (int w = 1; w < kWarps; ++w) {
+                const float4 y = xs[w][lane];
+                x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+                l += ls[w];
+            }
+            __syncthreads();
+        }
+        if (warp != 0) continue;
+        const int token = rec.token0 + r / A.G, head = rec.head * A.G + r % A.G;
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        *reinterpret_cast<uint2*>(A.o + token * A.o_token + head * A.o_head + 8 * lane) =
+            make_uint2(Pack2<T>::round(x.x * inv, x.y * inv), Pack2<T>::round(x.z * inv, x.w * inv));
+        if (A.lse != nullptr && lane == 0) A.lse[static_cast<int64_t>(token) * (A.Hkv * A.G) + head] = top * kLn2 + logf(l);
     }
-    const int token = rec.token0 + r / A.G, head = rec.head * A.G + r % A.G;
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    *reinterpret_cast<uint2*>(A.o + token * A.o_token + head * A.o_head + 8 * lane) =
-        make_uint2(Pack2<T>::round(x.x * inv, x.y * inv), Pack2<T>::round(x.z * inv, x.w * inv));
-    if (A.lse != nullptr && lane == 0) A.lse[static_cast<int64_t>(token) * (A.Hkv * A.G) + head] = top * kLn2 + logf(l);
 }
 
 // The driver's encoder: asked for once; the library is not linked against the driver, so that it loads where there is none.
@@ -88,7 +97,7 @@ struct PagedPlan {
 PagedPlan plan_paged(int64_t group_rows)
 {
     PagedPlan p;
-    p.rows = group_rows <= 16 ? 16 : 32;
+    p.rows = group_rows <= 16 ? 16 : group_rows <= 32 ? 32 : 2 * kChunkRows;
     p.ml = static_cast<size_t>(2 * kMaxCtas) * p.rows * kPagedD * 4;
     p.records = p.ml + static_cast<size_t>(2 * kMaxCtas) * p.rows * sizeof(float2);
     p.total = p.records + kMaxCtas * sizeof(PagedRecord);
@@ -112,7 +121,18 @@ cudaError_t launch_few_rows(const CUtensorMap& mq, const CUtensorMap& mk, const 
     constexpr int smem = static_cast<int>(sizeof(FewSmem<kM>)) + 1024;
     cudaError_t e = allow_smem(paged_few_kernel<T, kM>, smem, done, dev);
     if (e == cudaSuccess) e = launch_overlapped(paged_few_kernel<T, kM>, dim3(static_cast<unsigned>(ctas)), kFewThreads, smem, st, mq, mk, mv, A);
-    if (e == cudaSuccess) e = launch_overlapped(paged_join_kernel<T, 16 * kM>, dim3(static_cast<unsigned>(ctas), static_cast<unsigned>(max_rows)), 128, 0, st, A);
+    if (e == cudaSuccess) e = launch_overlapped(paged_join_kernel<T, 16 * kM, 4>, dim3(static_cast<unsigned>(ctas), static_cast<unsigned>(max_rows)), 128, 0, st, A, 16 * kM);
+    return e;
+}
+
+template <typename T>
+cudaError_t launch_chunk(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const PagedArgs& A, int ctas, int dev, cudaStream_t st)
+{
+    static std::atomic<uint64_t> done{0};
+    constexpr int smem = static_cast<int>(sizeof(ChunkSmem)) + 1024;
+    cudaError_t e = allow_smem(paged_chunk_kernel<T>, smem, done, dev);
+    if (e == cudaSuccess) e = launch_overlapped(paged_chunk_kernel<T>, dim3(static_cast<unsigned>(ctas)), kChunkThreads, smem, st, mq, mk, mv, A);
+    if (e == cudaSuccess) e = launch_overlapped(paged_join_kernel<T, 2 * kChunkRows, 1>, dim3(static_cast<unsigned>(ctas), 16), 128, 0, st, A, A.step / 2 * A.G);
     return e;
 }
 
@@ -125,7 +145,7 @@ efq_status_t paged_attention(const efq_rows_t* q, float* lse, int64_t total, int
     if (st != EFQ_OK) return st;
     if (q->heads % cache->n_heads != 0) return EFQ_ERR_INVALID_ARG;
     const int G = q->heads / cache->n_heads;
-    if (G > 32 || total >= (1ll << 31) - 256) return EFQ_ERR_UNSUPPORTED;
+    if (G > kChunkRows || total >= (1ll << 31) - 256) return EFQ_ERR_UNSUPPORTED;
     if (q->src_head < 0 || q->src_token < 0 || q->dst_head < 0 || q->dst_token < 0) return EFQ_ERR_INVALID_ARG;
     if (!aligned_rows(q->src, q->src_head, q->src_token, 0) || !aligned_rows(q->dst, q->dst_head, q->dst_token, 0)) return EFQ_ERR_ALIGNMENT;
     if ((reinterpret_cast<uintptr_t>(lse) & 3u) != 0) return EFQ_ERR_ALIGNMENT;
@@ -165,24 +185,28 @@ efq_status_t paged_attention(const efq_rows_t* q, float* lse, int64_t total, int
     A.part_ml = reinterpret_cast<float2*>(ws + plan.ml);
     A.records = reinterpret_cast<PagedRecord*>(ws + plan.records);
     A.inject_skip_loads = inject_skip_loads ? 1 : 0;
-    A.step = plan.rows / G > 0 ? plan.rows / G : 1;
+    const bool many = plan.rows > 32;
+    A.step = many ? kChunkRows / G * 2 : plan.rows / G;
 
     CUtensorMap mq, mk, mv;
     const uint64_t q_dims[3] = {kPagedD, static_cast<uint64_t>(q->heads), static_cast<uint64_t>(total)};
     const int64_t q_strides[2] = {q->src_head, q->src_token};
-    const uint32_t q_box[3] = {64, static_cast<uint32_t>(G), static_cast<uint32_t>(A.step)};
+    const uint32_t q_box[3] = {64, static_cast<uint32_t>(G), static_cast<uint32_t>(many ? A.step / 2 : A.step)};
     const uint64_t dims[4] = {kPagedD, static_cast<uint64_t>(cache->page_size), static_cast<uint64_t>(cache->n_heads), static_cast<uint64_t>(cache->n_pages)};
     const int64_t k_strides[3] = {cache->k_token, cache->k_head, cache->k_page}, v_strides[3] = {cache->v_token, cache->v_head, cache->v_page};
-    const uint32_t box[4] = {64, static_cast<uint32_t>(cache->page_size < kFewKeys ? cache->page_size : kFewKeys), 1, 1};
+    const int keys = many ? kChunkKeys : kFewKeys;
+    const uint32_t box[4] = {64, static_cast<uint32_t>(cache->page_size < keys ? cache->page_size : keys), 1, 1};
     if (!encode_rows(&mq, dtype, q->src, 3, q_dims, q_strides, q_box) || !encode_rows(&mk, dtype, cache->k, 4, dims, k_strides, box) ||
         !encode_rows(&mv, dtype, cache->v, 4, dims, v_strides, box))
         return EFQ_ERR_CUDA;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const int max_rows = A.step * G;
     using Bf = __nv_bfloat16;
-    const cudaError_t e = dtype == EFQ_BF16
-        ? (plan.rows == 16 ? launch_few_rows<Bf, 1>(mq, mk, mv, A, ctas, max_rows, dev, s) : launch_few_rows<Bf, 2>(mq, mk, mv, A, ctas, max_rows, dev, s))
-        : (plan.rows == 16 ? launch_few_rows<__half, 1>(mq, mk, mv, A, ctas, max_rows, dev, s) : launch_few_rows<__half, 2>(mq, mk, mv, A, ctas, max_rows, dev, s));
+    const bool bf = dtype == EFQ_BF16;
+    const cudaError_t e = many ? (bf ? launch_chunk<Bf>(mq, mk, mv, A, ctas, dev, s) : launch_chunk<__half>(mq, mk, mv, A, ctas, dev, s))
+                          : plan.rows == 16
+                              ? (bf ? launch_few_rows<Bf, 1>(mq, mk, mv, A, ctas, max_rows, dev, s) : launch_few_rows<__half, 1>(mq, mk, mv, A, ctas, max_rows, dev, s))
+                              : (bf ? launch_few_rows<Bf, 2>(mq, mk, mv, A, ctas, max_rows, dev, s) : launch_few_rows<__half, 2>(mq, mk, mv, A, ctas, max_rows, dev, s));
     return e == cudaSuccess ? EFQ_OK : EFQ_ERR_CUDA;
 }
 

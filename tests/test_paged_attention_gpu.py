@@ -50,6 +50,7 @@ CHUNK = [
     ([(50, 51)], 3, 1, 16),
     ([(2000, 2100)], 2, 2, 128), ([(1, 700), (300, 400), (5, 2000), (0, 10), (128, 128), (1, 1), (40, 999)], 8, 2, 16),
     ([(37, 37 + 100 * i) for i in range(20)], 4, 2, 64), ([(1024, 1024)], 4, 4, 512),
+    ([(1, 640)], 64, 1, 16), ([(2, 333)], 128, 1, 16), ([(1, 1)], 128, 1, 16), ([(3, 100)], 50, 1, 32), ([(5, 64)], 33, 1, 16),
 ]
 
 
