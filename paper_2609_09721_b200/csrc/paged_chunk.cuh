@@ -1,8 +1,8 @@
 // Attention over a paged cache for many query rows: 128 or 256 rows of a KV group against tiles of 128 keys, on the tensor cores.
 //
 // A query tile is two halves of up to 128 rows (tokens of the chunk times the query heads of the KV group, whole tokens only), each with
-// its scores (128 columns of tensor memory, whose first 64 take the probabilities afterwards) and its output (128 columns).  Ten warps: four
-// for the softmax of each half, one that issues the MMAs, one that loads (and two that fill their group of four).  While the softmax warps of one half are busy, the tensor core
+// its scores (128 columns of tensor memory, whose first 64 take the probabilities afterwards) and its output (128 columns).  Twelve warps: four
+// for the softmax of each half, one for each half that issues its MMAs, one that loads, one that clears rows of V past a sequence.  While the softmax warps of one half are busy, the tensor core
 // has the other half's products: per half and tile Q K^T (both operands in shared memory), then P V (P from tensor memory).
 //   - A thread has a row, so maxima and sums need no other thread.  The output is rescaled in tensor memory by the same threads,
 //     only when a row's maximum has grown by more than 2^8 (kSlack); the sum refers to the same maximum, so the result is exact.  When
@@ -16,7 +16,7 @@
 
 namespace efq {
 
-constexpr int kChunkKeys = 128, kChunkRows = 128;              // keys of a tile, rows of a half
+constexpr int kChunkShift = 7, kChunkKeys = 1 << kChunkShift, kChunkRows = 128;      // keys of a tile, rows of a half
 constexpr int kChunkThreads = 384;
 constexpr int kChunkSlots = 5;
 constexpr int kChunkPart = kChunkKeys * 128;                   // bytes of 64 channels of 128 rows
@@ -26,9 +26,9 @@ constexpr float kSlack = 8.0f;                                 // log2: probabil
 struct __align__(1024) ChunkSmem {
     uint8_t q[2][2][kChunkPart];                               // half, channels 0-63 and 64-127; 128-byte swizzle
     uint8_t kv[kChunkSlots][2][kChunkPart];
-    uint64_t full[kChunkSlots], empty[kChunkSlots], q_full, q_empty, s_full[2], p_ready[2], o_full[2], drained;
+    uint64_t full[kChunkSlots], empty[kChunkSlots], q_full, q_empty, s_full[2], p_ready[2], p_rest[2], o_full[2], v_tail, v_clean, turn[2], drained[2];
     int64_t scratch[kChunkThreads / 32];
-    PagedRun run;
+    PagedRun<kChunkShift> run;
     uint32_t tmem_base;
     volatile uint32_t failed;
 };
@@ -43,17 +43,66 @@ __device__ constexpr uint32_t chunk_idesc(bool b_n_major)
     return __is_same(T, __nv_bfloat16) ? ptx::bf16_idesc(128, b_n_major) : ptx::bf16_idesc(128, b_n_major) & ~((1u << 7) | (1u << 10));
 }
 
+// Two FP32 operations in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 d;
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\tfma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    float2 d;
+    asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+// NaN if one of them is
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float d;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+// 2^x for x <= 8 on the FMA pipe: x = n + f with n the nearest integer, 1 + f q(f) with q of degree 3 fitted to the smallest relative error on
+// [-1/2, 1/2] (least squares, reweighted until the error is level: 2.9e-6, a thousandth of what rounding the probability costs), n added
+// to the exponent.  Below -127 the result is 0, exactly: f = 0 there and the exponent field is empty.  NaN is not kept.
+__device__ __forceinline__ float2 poly_exp2(float2 x)
+{
+    constexpr float kMagic = 12582912.0f;           // 1.5 * 2^23: adding it leaves the integer in the low bits
+    x = make_float2(fmaxf(x.x, -127.0f), fmaxf(x.y, -127.0f));
+    const float2 t = add2(x, make_float2(kMagic, kMagic)), n = add2(t, make_float2(-kMagic, -kMagic));
+    const float2 f = fma2(n, make_float2(-1.0f, -1.0f), x);
+    float2 y = fma2(f, make_float2(9.582852944731712e-3f, 9.582852944731712e-3f), make_float2(5.5906426161527634e-2f, 5.5906426161527634e-2f));
+    y = fma2(f, y, make_float2(0.24024099111557007f, 0.24024099111557007f));
+    y = fma2(f, y, make_float2(0.6931241750717163f, 0.6931241750717163f));
+    y = fma2(f, y, make_float2(1.0f, 1.0f));
+    return make_float2(__uint_as_float(__float_as_uint(y.x) + (__float_as_uint(t.x) << 23)), __uint_as_float(__float_as_uint(y.y) + (__float_as_uint(t.y) << 23)));
+}
+// 16 registers into 16 columns of tensor memory
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
+                 ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+                 "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr) : "memory");
+}
+
+// Tells the compiler that a value is the same in all lanes.
+template <typename V>
+__device__ __forceinline__ V uniform(V x) { return __shfl_sync(0xffffffffu, x, 0); }
+
 // Of a segment: tokens of a half, and the key tiles of the run that it needs: [j0, end).
 struct ChunkHalf {
     int tokens, end;
 };
-__device__ __forceinline__ ChunkHalf chunk_half(const PagedSegment& g, int half, int step)
+__device__ __forceinline__ ChunkHalf chunk_half(const PagedSegment<kChunkShift>& g, int half, int step)
 {
     const int per = step >> 1;
     ChunkHalf h;
     h.tokens = max(0, min(per, g.tokens - half * per));
     const int seen = h.tokens > 0 ? paged_limit(g, half * per + h.tokens - 1) : 0;
-    h.end = max(g.j0, min(g.j1, (seen + kChunkKeys - 1) / kChunkKeys));
+    h.end = max(g.j0, min(g.j1, (seen + kChunkKeys - 1) >> kChunkShift));
     return h;
 }
 
@@ -64,20 +113,24 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
 {
     extern __shared__ uint8_t smem_raw[];
     ChunkSmem* const sm = reinterpret_cast<ChunkSmem*>(smem_raw + ptx::smem_round_up(smem_raw, 1024u));
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
     if (tid == 0) {
         sm->failed = 0u;
         for (int i = 0; i < kChunkSlots; ++i) {
             ptx::mbar_init(&sm->full[i], 1);
-            ptx::mbar_init(&sm->empty[i], 1);
+            ptx::mbar_init(&sm->empty[i], 2);
         }
         ptx::mbar_init(&sm->q_full, 1);
-        ptx::mbar_init(&sm->q_empty, 1);
-        ptx::mbar_init(&sm->drained, 1);
+        ptx::mbar_init(&sm->q_empty, 2);
+        ptx::mbar_init(&sm->v_tail, 1);
+        ptx::mbar_init(&sm->v_clean, 1);
         for (int i = 0; i < 2; ++i) {
             ptx::mbar_init(&sm->s_full[i], 1);
             ptx::mbar_init(&sm->p_ready[i], 4);
+            ptx::mbar_init(&sm->p_rest[i], 4);
             ptx::mbar_init(&sm->o_full[i], 1);
+            ptx::mbar_init(&sm->drained[i], 1);
+            ptx::mbar_init(&sm->turn[i], 1);
         }
         ptx::mbar_init_fence();
         ptx::prefetch_tensormap(&mq);
@@ -88,11 +141,11 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
     ptx::tc_fence_before_sync();
     ptx::grid_wait();
     ptx::grid_launch_next();
-    paged_find_run<kChunkThreads, kChunkKeys>(A, sm->scratch, &sm->run);      // two barriers of the block
+    paged_find_run<kChunkThreads, kChunkShift>(A, sm->scratch, &sm->run);      // two barriers of the block
     ptx::tc_fence_after_sync();
     const uint32_t tmem = sm->tmem_base;
-    PagedWalk<PagedReader<kChunkKeys>> walk(PagedReader<kChunkKeys>{A}, A.n_seqs, A.Hkv, sm->run);
-    PagedSegment g;
+    PagedWalk<kChunkShift, PagedReader<kChunkShift>> walk(PagedReader<kChunkShift>{A}, A.n_seqs, A.Hkv, sm->run);
+    PagedSegment<kChunkShift> g;
 
     if (warp >= 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kChunkRegsLess));
@@ -104,22 +157,25 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
             while (ok && walk.next(g)) {
                 const int end = max(chunk_half(g, 0, A.step).end, chunk_half(g, 1, A.step).end);
                 const int32_t* table = A.page_table + g.seq * A.table_stride;
+                // as it stands in the table: it is looked at when the tile after the next is loaded, so that nobody waits for it here
                 auto entry_of = [&](int j) {
                     const int key = j * kChunkKeys + row, at = key >> A.page_shift;
                     int e = -1;
-                    if (row < kChunkKeys && key < g.w.len && at < A.max_pages) e = __ldcg(table + at);
-                    return e < A.n_pages ? e : -1;
+                    if (row < kChunkKeys && j < end && key < g.w.len) e = __ldcg(table + at);
+                    return e;
                 };
                 // One operand of a tile: lane i takes its i-th page.  Where an entry is no page, the rows of K are NaN, which makes rows of
                 // NaN of the queries that see them, and the rows of V are 0.
-                auto load = [&](const CUtensorMap& map, int j, int entry, uint32_t fill) {
+                auto load = [&](const CUtensorMap& map, int j, int at, uint32_t fill) {
+                    const int entry = at < A.n_pages ? at : -1;
                     const uint32_t s = slot % kChunkSlots;
                     if (slot >= kChunkSlots) ok = paged_wait_warp(&sm->empty[s], (slot / kChunkSlots - 1) & 1u, sm);
                     if (!ok) return;
                     const int key = j * kChunkKeys + row;
                     const bool mine = row < kChunkKeys && key < g.w.len, page = mine && entry >= 0 && !A.inject_skip_loads;
                     if (mine && entry < 0) {
-                        for (int i = 0; i < box * 8; ++i) {
+    #pragma unroll 1
+                    for (int i = 0; i < box * 8; ++i) {
                             reinterpret_cast<uint4*>(sm->kv[s][0] + row * 128)[i] = make_uint4(fill, fill, fill, fill);
                             reinterpret_cast<uint4*>(sm->kv[s][1] + row * 128)[i] = make_uint4(fill, fill, fill, fill);
                         }
@@ -134,9 +190,9 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
                     }
                     ++slot;
                 };
-                int entry = end > g.j0 ? entry_of(g.j0) : -1;
+                int entry = entry_of(g.j0), next = entry_of(g.j0 + 1);
                 for (int j = g.j0; ok && j < end; ++j) {
-                    const int ahead = j + 1 < end ? entry_of(j + 1) : -1;
+                    const int ahead = entry_of(j + 2);
                     load(mk, j, entry, 0x7fff7fffu);
                     if (ok && j == g.j0) {
                         if (q_loads > 0) ok = paged_wait_warp(&sm->q_empty, (q_loads - 1) & 1u, sm);
@@ -151,7 +207,8 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
                         ++q_loads;
                     }
                     if (ok) load(mv, j, entry, 0u);
-                    entry = ahead;
+                    entry = next;
+                    next = ahead;
                 }
             }
             if (lane == 0) {        // its copies in flight end before the block does, whatever the others do
@@ -161,88 +218,156 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
                 }
                 for (int n = 0; n < 20000 && q_loads > 0 && !ptx::mbar_try_wait_suspend(&sm->q_full, (q_loads - 1) & 1u, 50000u); ++n) {}
             }
-        } else if (warp == 8) {
-            // ------------------------------------------------------------ MMAs
-            uint32_t slot = 0, q_loads = 0, p_count[2] = {0, 0};
-            bool ok = true;
-            auto wait_slot = [&](uint32_t s) { return paged_wait_warp(&sm->full[s % kChunkSlots], (s / kChunkSlots) & 1u, sm); };
-            auto scores = [&](int w, uint32_t s) {
-                const uint64_t da = ptx::smem_desc(ptx::smem_u32(sm->q[w][0]), 16, 1024, ptx::kLayoutSw128);
-                const uint64_t db = ptx::smem_desc(ptx::smem_u32(sm->kv[s % kChunkSlots][0]), 16, 1024, ptx::kLayoutSw128);
-                if (ptx::elect_one()) {
-    #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const uint64_t off = static_cast<uint64_t>(((i >> 2) * kChunkPart + (i & 3) * 32) >> 4);
-                        ptx::mma_bf16(tmem + kChunkColS + 128 * w, da + off, db + off, chunk_idesc<T>(false), i > 0 ? 1u : 0u);
-                    }
-                    ptx::mma_commit(&sm->s_full[w]);
+        } else if (warp != 10) {
+            // ------------------------------------------------------------ MMAs: warp 8 the first half's, warp 11 the second's
+            // The tensor core's queue holds four of these products, 64 clocks each: what a warp does between two of them must not take
+            // longer.  So the whole warp walks, on values that the compiler knows to be the same in all lanes (uniform registers, no moves for
+            // each operand; a single thread's loop took 1170 to 1530 clocks for 16 products beside busy warps, this one 1030 to 1040), and
+            // what one half waits for does not hold up the other.  Every tile of the run is walked by both, so that a slot is free when
+            // both have let it go.
+            const int w = uniform(warp == 11 ? 1 : 0);
+            const uint32_t tm = uniform(tmem), s_tmem = tm + kChunkColS + 128 * w, o_tmem = tm + kChunkColO + 128 * w;
+            const uint64_t dq = ptx::smem_desc(ptx::smem_u32(sm->q[0][0]) + w * 2 * kChunkPart, 16, 1024, ptx::kLayoutSw128);
+            const uint64_t dk = ptx::smem_desc(ptx::smem_u32(sm->kv[0][0]), 16, 1024, ptx::kLayoutSw128);
+            const uint64_t dv = ptx::smem_desc(ptx::smem_u32(sm->kv[0][0]), kChunkPart, 1024, ptx::kLayoutSw128);
+            constexpr uint32_t kSlotStep = 2 * kChunkPart >> 4;
+            uint64_t *const s_full = &sm->s_full[w], *const p_ready = &sm->p_ready[w], *const p_rest = &sm->p_rest[w], *const o_full = &sm->o_full[w];
+            uint64_t *const turn_mine = &sm->turn[w], *const turn_other = &sm->turn[w ^ 1];
+            uint32_t slot = 0, round = 0, q_round = 0, p_round = 0, clean_round = 0, turn_round = 0;        // parities of the next waits
+            bool ok = true, first = w == 0;         // nobody is before the first half's first turn
+            auto advance = [&]() {
+                if (++slot == kChunkSlots) {
+                    slot = 0;
+                    round ^= 1u;
                 }
-                __syncwarp();
+            };
+            // The halves take turns, the first one first: while one has its products the other has its softmax.  Left to themselves they fall
+            // into step, both at the exponentials and then both at the tensor core.
+            auto my_turn = [&]() {
+                if (first) {
+                    first = false;
+                    return true;
+                }
+                const bool there = paged_wait_warp(turn_mine, turn_round, sm);
+                turn_round ^= 1u;
+                return there;
+            };
+            // one thread's; hands over before the last products, which the queue holds until the other warp is there
+            auto scores = [&]() {
+                const uint64_t k = dk + slot * kSlotStep;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t off = ((i >> 2) * kChunkPart + (i & 3) * 32) >> 4;
+                    ptx::mma_bf16(s_tmem, dq + off, k + off, chunk_idesc<T>(false), i > 0 ? 1u : 0u);
+                    if (i == 4) ptx::mbar_arrive(turn_other);
+                }
+                ptx::mma_commit(s_full);
+                ptx::mma_commit(&sm->empty[slot]);
             };
             while (ok && walk.next(g)) {
-                const int e0 = chunk_half(g, 0, A.step).end, e1 = chunk_half(g, 1, A.step).end, end = max(e0, e1);
-                if (end == g.j0) continue;
-                ok = wait_slot(slot) && paged_wait_warp(&sm->q_full, q_loads & 1u, sm);
+                const int e0 = chunk_half(g, 0, A.step).end, e1 = chunk_half(g, 1, A.step).end;
+                const int j0 = uniform(g.j0), mine = uniform(w ? e1 : e0), end = uniform(max(e0, e1)), clean = uniform(g.w.len < max(e0, e1) * kChunkKeys ? 1 : 0);
+                if (end == j0) continue;
+                ok = paged_wait_warp(&sm->q_full, q_round, sm) && paged_wait_warp(&sm->full[slot], round, sm);
+                q_round ^= 1u;
                 if (!ok) break;
-                ++q_loads;
-                ptx::tc_fence_after_sync();
-                if (g.j0 < e0) scores(0, slot);
-                if (g.j0 < e1) scores(1, slot);
+                // the first scores
+                ok = my_turn();
+                if (!ok) break;
                 if (ptx::elect_one()) {
-                    ptx::mma_commit(&sm->empty[slot % kChunkSlots]);
-                    if (g.j0 + 1 == end) ptx::mma_commit(&sm->q_empty);
+                    if (j0 < mine) {
+                        scores();
+                    } else {
+                        ptx::mbar_arrive(turn_other);
+                        ptx::mbar_arrive(&sm->empty[slot]);
+                    }
+                    if (j0 + 1 == end) ptx::mma_commit(&sm->q_empty);
                 }
                 __syncwarp();
-                ++slot;
-                for (int j = g.j0; ok && j < end; ++j) {
-                    const uint32_t v_slot = slot, k_slot = slot + 1;
-                    const bool more = j + 1 < end;
-                    ok = wait_slot(v_slot) && (!more || wait_slot(k_slot));
-                    if (!ok) break;
-                    slot += more ? 2 : 1;
-                    const int inside = g.w.len - j * kChunkKeys;
-                    if (inside < kChunkKeys) {      // rows of V past the sequence hold whatever the page held: 0 times that has to be 0
-                        uint8_t* const v = sm->kv[v_slot % kChunkSlots][0];
-                        for (int i = inside * 8 + lane; i < kChunkKeys * 8; i += 32) {
-                            reinterpret_cast<uint4*>(v)[i] = make_uint4(0u, 0u, 0u, 0u);
-                            reinterpret_cast<uint4*>(v + kChunkPart)[i] = make_uint4(0u, 0u, 0u, 0u);
-                        }
-                        ptx::fence_proxy_async_smem();
+                advance();
+                for (int j = j0; j < end; ++j) {
+                    const uint32_t v_slot = slot;
+                    ok = paged_wait_warp(&sm->full[slot], round, sm);
+                    advance();
+                    if (clean && j + 1 == end) {
+                        if (w == 0 && ptx::elect_one()) ptx::mbar_arrive(&sm->v_tail);
                         __syncwarp();
+                        ok = ok && paged_wait_warp(&sm->v_clean, clean_round, sm);
+                        clean_round ^= 1u;
                     }
-                    const uint64_t dv = ptx::smem_desc(ptx::smem_u32(sm->kv[v_slot % kChunkSlots][0]), kChunkPart, 1024, ptx::kLayoutSw128);
-    #pragma unroll
-                    for (int w = 0; w < 2; ++w) {
-                        const int e = w == 0 ? e0 : e1;
-                        if (!ok || j >= e) continue;
-                        ok = paged_wait_warp(&sm->p_ready[w], p_count[w] & 1u, sm);
-                        if (!ok) continue;
-                        ++p_count[w];
+                    const bool more = j + 1 < end;
+                    if (more) ok = ok && paged_wait_warp(&sm->full[slot], round, sm);
+                    if (j < mine) {
+                        const uint64_t v = dv + v_slot * kSlotStep;
+                        ok = ok && paged_wait_warp(p_ready, p_round, sm) && my_turn();
+                        if (!ok) break;
                         ptx::tc_fence_after_sync();
                         if (ptx::elect_one()) {
-    #pragma unroll
-                            for (int i = 0; i < 8; ++i)
-                                ptx::mma_bf16_ts(tmem + kChunkColO + 128 * w, tmem + kChunkColS + 128 * w + 8 * i, dv + static_cast<uint64_t>(i * 2048 >> 4),
-                                                 chunk_idesc<T>(true), i > 0 || j > g.j0 ? 1u : 0u);
-                            if (j + 1 == e) ptx::mma_commit(&sm->o_full[w]);
+#pragma unroll
+                            for (int i = 0; i < 6; ++i)
+                                ptx::mma_bf16_ts(o_tmem, s_tmem + 8 * i, v + (i * 2048u >> 4), chunk_idesc<T>(true), i > 0 || j > j0 ? 1u : 0u);
                         }
                         __syncwarp();
-                        if (j + 1 < e) scores(w, k_slot);
+                        ok = paged_wait_warp(p_rest, p_round, sm);
+                        p_round ^= 1u;
+                        if (!ok) break;
+                        ptx::tc_fence_after_sync();
+                        if (ptx::elect_one()) {
+#pragma unroll
+                            for (int i = 6; i < 8; ++i) ptx::mma_bf16_ts(o_tmem, s_tmem + 8 * i, v + (i * 2048u >> 4), chunk_idesc<T>(true), 1u);
+                            if (j + 1 < mine) {
+                                scores();
+                            } else {
+                                ptx::mma_commit(o_full);
+                                ptx::mbar_arrive(turn_other);
+                                if (more) ptx::mbar_arrive(&sm->empty[slot]);
+                            }
+                            ptx::mma_commit(&sm->empty[v_slot]);
+                            if (j + 2 == end) ptx::mma_commit(&sm->q_empty);
+                        }
+                        __syncwarp();
+                    } else {
+                        ok = ok && my_turn();
+                        if (!ok) break;
+                        if (ptx::elect_one()) {
+                            ptx::mbar_arrive(turn_other);
+                            ptx::mbar_arrive(&sm->empty[v_slot]);
+                            if (more) ptx::mbar_arrive(&sm->empty[slot]);
+                            if (j + 2 == end) ptx::mma_commit(&sm->q_empty);
+                        }
+                        __syncwarp();
                     }
-                    if (!ok) break;
-                    if (ptx::elect_one()) {
-                        ptx::mma_commit(&sm->empty[v_slot % kChunkSlots]);
-                        if (more) ptx::mma_commit(&sm->empty[k_slot % kChunkSlots]);
-                        if (j + 2 == end) ptx::mma_commit(&sm->q_empty);
-                    }
-                    __syncwarp();
+                    if (more) advance();
                 }
             }
             if (!ok) {              // the MMAs that were issued end before tensor memory is given back
-                if (ptx::elect_one()) ptx::mma_commit(&sm->drained);
+                if (ptx::elect_one()) ptx::mma_commit(&sm->drained[w]);
                 __syncwarp();
-                for (int n = 0; n < 20000 && !ptx::mbar_try_wait_suspend(&sm->drained, 0u, 50000u); ++n) {}
+                for (int n = 0; n < 20000 && !ptx::mbar_try_wait_suspend(&sm->drained[w], 0u, 50000u); ++n) {}
                 __syncwarp();
+            }
+        } else if (warp == 10) {
+            // ------------------------------------------------------------ rows of V past a sequence
+            // They hold whatever the page held, and 0 times that has to be 0.
+            uint32_t slot = 0, round = 0;           // loads so far; parity of the next wait
+            bool ok = true;
+            while (ok && walk.next(g)) {
+                const int end = max(chunk_half(g, 0, A.step).end, chunk_half(g, 1, A.step).end), inside = g.w.len - (end - 1) * kChunkKeys;
+                if (end == g.j0) continue;
+                slot += 2 * (end - g.j0);
+                if (inside >= kChunkKeys) continue;
+                ok = paged_wait_warp(&sm->v_tail, round, sm);
+                if (!ok) break;
+                round ^= 1u;
+                uint8_t* const v = sm->kv[(slot - 1) % kChunkSlots][0];
+#pragma unroll 1
+                for (int i = inside * 8 + lane; i < kChunkKeys * 8; i += 32) {
+                    reinterpret_cast<uint4*>(v)[i] = make_uint4(0u, 0u, 0u, 0u);
+                    reinterpret_cast<uint4*>(v + kChunkPart)[i] = make_uint4(0u, 0u, 0u, 0u);
+                }
+                ptx::fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(&sm->v_clean);
             }
         }
     } else {
@@ -276,19 +401,23 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
 #pragma unroll
                     for (int c = 0; c < 128; ++c) s[c] = c < seen ? s[c] : -INFINITY;
                 }
-                float top[4];
+                float top[8];
 #pragma unroll
-                for (int c = 0; c < 4; ++c) top[c] = s[c];
+                for (int c = 0; c < 8; ++c) top[c] = s[c];
 #pragma unroll
-                for (int c = 4; c < 128; ++c) top[c & 3] = fmaxf(top[c & 3], s[c]);
-                const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * A.scale_log2;
-                const bool grew = mx > m + kSlack || (m == -INFINITY && mx > m);
+                for (int c = 8; c < 120; c += 16)
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) top[q] = max3(top[q], s[c + q], s[c + 8 + q]);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) top[q] = max3(top[q], s[120 + q], top[q]);
+                const float mx = max3(max3(top[0], top[1], top[2]), max3(top[3], top[4], top[5]), max3(top[6], top[7], top[7])) * A.scale_log2;
+                const bool grew = !(mx <= m + kSlack);        // also a NaN
                 if (__any_sync(0xffffffffu, grew)) {
                     const float alpha = grew ? (m == -INFINITY ? 0.0f : paged_exp2(m - mx)) : 1.0f;
-                    if (grew) m = mx;
+                    if (grew) m = mx < INFINITY ? mx : __uint_as_float(0x7fc00000u);      // an infinite score makes a row of NaN, as inf - inf does
                     l *= alpha;
                     if (j > g.j0) {
-#pragma unroll
+#pragma unroll 1
                         for (int q = 0; q < 4; ++q) {
                             float o[32];
                             uint32_t u[32];
@@ -301,25 +430,33 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
                     }
                 }
                 const float base = m == -INFINITY ? 0.0f : m;        // nothing visible yet: every exponential is 2^-inf = 0
-                float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                const float2 scale2 = make_float2(A.scale_log2, A.scale_log2), minus2 = make_float2(-base, -base);
+                float2 sum2[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    uint32_t p[32];
+                for (int q = 0; q < 4; ++q) {
+                    uint32_t p[16];
 #pragma unroll
-                    for (int c = 0; c < 32; ++c) {
-                        const float p0 = paged_exp2(fmaf(s[64 * q + 2 * c], A.scale_log2, -base)), p1 = paged_exp2(fmaf(s[64 * q + 2 * c + 1], A.scale_log2, -base));
-                        sum[(2 * c) & 3] += p0;
-                        sum[(2 * c + 1) & 3] += p1;
+                    for (int c = 0; c < 16; ++c) {
+                        if (q == 3 && c == 8) {          // the product with V begins while the last quarter is made
+                            ptx::tmem_wait_st();
+                            ptx::tc_fence_before_sync();
+                            __syncwarp();
+                            if (lane == 0) ptx::mbar_arrive(&sm->p_ready[w]);
+                        }
+                        float2 y = fma2(make_float2(s[32 * q + 2 * c], s[32 * q + 2 * c + 1]), scale2, minus2);
+                        y = c % 4 == 3 ? poly_exp2(y) : make_float2(paged_exp2(y.x), paged_exp2(y.y));
+                        sum2[c & 1] = add2(sum2[c & 1], y);
                         // rounded once, to the elements' type (half a step of 2^-8 or 2^-11 of each); the sum is kept unrounded
-                        p[c] = Pack2<T>::round(p0, p1);
+                        p[c] = Pack2<T>::round(y.x, y.y);
                     }
-                    ptx::tmem_st32<0>(s_col + 32 * q, p);
+                    tmem_st16(s_col + 16 * q, p);        // over scores that have been read
                 }
-                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
                 ptx::tmem_wait_st();
                 ptx::tc_fence_before_sync();
                 __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(&sm->p_ready[w]);
+                if (lane == 0) ptx::mbar_arrive(&sm->p_rest[w]);
+                sum2[0] = add2(sum2[0], sum2[1]);
+                l += sum2[0].x + sum2[0].y;
             }
 
             const bool some = h.end > g.j0, all = g.j0 == 0 && g.j1 == g.n;
@@ -333,7 +470,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
             const float inv = l == 0.0f ? 0.0f : 1.0f / l;
             char* const dst = A.o + token * A.o_token + head * A.o_head;
             float4* const part = reinterpret_cast<float4*>(A.part_o + (static_cast<int64_t>(slot) * 2 * kChunkRows + w * kChunkRows + r) * kPagedD);
-#pragma unroll
+#pragma unroll 1
             for (int q = 0; q < 4; ++q) {
                 float o[32];
                 if (some && !nan) {

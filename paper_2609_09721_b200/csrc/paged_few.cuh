@@ -13,7 +13,7 @@
 
 namespace efq {
 
-constexpr int kFewKeys = 64;                    // of a stage
+constexpr int kFewShift = 6, kFewKeys = 1 << kFewShift;       // of a stage
 constexpr int kFewWarps = 8;                    // that compute
 constexpr int kFewThreads = (kFewWarps + 1) * 32;
 constexpr int kFewHalf = kFewKeys * 128;        // bytes of 64 channels of a tile
@@ -32,21 +32,26 @@ struct __align__(1024) FewSmem {
     float2 row_ml[16 * kM];
     uint64_t full[kStages], empty[kStages], q_full[2], q_empty[2];
     int64_t scratch[64];
-    PagedRun run;
+    PagedRun<kFewShift> run;
     uint32_t bad[kStages];                      // the tile lies on an entry that is no page
     volatile uint32_t failed;
 };
 
+// Bounded waits.
+__device__ __forceinline__ bool paged_poll(uint64_t* bar, uint32_t parity, volatile uint32_t* failed)
+{
+#pragma unroll 1
+    for (int i = 0; i < 20000; ++i) {           // a second at most
+        if (*failed != 0u) return false;
+        if (ptx::mbar_try_wait_suspend(bar, parity, 50000u)) return true;
+    }
+    *failed = 1u;
+    return false;
+}
 template <typename Smem>
 __device__ __forceinline__ bool paged_wait(uint64_t* bar, uint32_t parity, Smem* sm)
 {
-    if (ptx::mbar_try_wait(bar, parity)) return true;
-    for (int i = 0; i < 20000; ++i) {           // a second at most
-        if (sm->failed != 0u) return false;
-        if (ptx::mbar_try_wait_suspend(bar, parity, 50000u)) return true;
-    }
-    sm->failed = 1u;
-    return false;
+    return ptx::mbar_try_wait(bar, parity) || paged_poll(bar, parity, &sm->failed);
 }
 
 // The same for a warp, whose lanes leave the wait together: what follows needs all of them (ldmatrix, mma, ballots).
@@ -89,7 +94,7 @@ __device__ __forceinline__ void few_bar() { asm volatile("bar.sync 1, 256;" ::: 
 
 // Loads of one tile: lane i takes the i-th page of it.  `entry`: that page's entry in the table (below zero where it is none).
 template <int kStages, typename Smem>
-__device__ __forceinline__ void few_load_tile(Smem* sm, int stage, const CUtensorMap& mk, const CUtensorMap& mv, const PagedArgs& A, const PagedSegment& g,
+__device__ __forceinline__ void few_load_tile(Smem* sm, int stage, const CUtensorMap& mk, const CUtensorMap& mv, const PagedArgs& A, const PagedSegment<kFewShift>& g,
                                               int j, int entry, int lane)
 {
     const int P = 1 << A.page_shift, box = min(P, kFewKeys), key = j * kFewKeys + lane * box;
@@ -137,9 +142,9 @@ paged_few_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
     }
     ptx::grid_wait();
     ptx::grid_launch_next();
-    paged_find_run<kFewThreads, kFewKeys>(A, sm->scratch, &sm->run);      // two barriers of the block
-    PagedWalk<PagedReader<kFewKeys>> walk(PagedReader<kFewKeys>{A}, A.n_seqs, A.Hkv, sm->run);
-    PagedSegment g;
+    paged_find_run<kFewThreads, kFewShift>(A, sm->scratch, &sm->run);      // two barriers of the block
+    PagedWalk<kFewShift, PagedReader<kFewShift>> walk(PagedReader<kFewShift>{A}, A.n_seqs, A.Hkv, sm->run);
+    PagedSegment<kFewShift> g;
 
     if (warp == kFewWarps) {
         // ------------------------------------------------------------ loads

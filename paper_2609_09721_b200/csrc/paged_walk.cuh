@@ -30,39 +30,36 @@ struct PagedRecord {
     int32_t token0, tokens, head;
 };
 
-// Sequence s of the step as a kernel with tiles of kKeys keys sees it.
-template <int kKeys>
+// Sequence s of the step.
+template <int kShift>
 struct PagedReader {
     const PagedArgs& A;
-    __device__ __forceinline__ SeqWork operator()(int s, int& begin) const
+    __device__ __forceinline__ void operator()(int s, SeqWork<kShift>& w, int& begin) const
     {
-        SeqWork w;
         begin = __ldcg(A.cu_seqlens + s);
-        w.lq = __ldcg(A.cu_seqlens + s + 1) - begin;
-        w.len = max(0, __ldcg(A.seq_lens + s));
-        if (begin < 0 || w.lq < 0 || begin > A.total - w.lq) w.lq = 0;      // not tokens of this step: nothing is read or written for it
-        if (w.len > A.max_pages << A.page_shift) {
-            w.none = 1;
-            w.len = 0;
-        }
-        w.step = A.step;
-        w.keys = kKeys;
-        w.causal = A.causal;
-        return w;
+        int lq = __ldcg(A.cu_seqlens + s + 1) - begin, len = max(0, __ldcg(A.seq_lens + s));
+        if (begin < 0 || lq < 0 || begin > A.total - lq) lq = 0;      // not tokens of this step: nothing is read or written for it
+        const bool none = len > A.max_pages << A.page_shift;
+        w.set(lq, none ? 0 : len, A.step, A.causal, none ? 1 : 0);
     }
 };
 
 // Called by all kThreads threads of a CTA; `scratch` holds a number for each of its warps, in shared memory.
-template <int kThreads, int kKeys>
-__device__ __forceinline__ void paged_find_run(const PagedArgs& A, int64_t* scratch, PagedRun* run)
+template <int kThreads, int kShift>
+__device__ __noinline__ void paged_find_run(const PagedArgs& A, int64_t* scratch, PagedRun<kShift>* run)
 {
-    const PagedReader<kKeys> read{A};
+    const PagedReader<kShift> read{A};
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     constexpr int kWarps = kThreads / 32;
     const int per = (A.n_seqs + kThreads - 1) / kThreads, s0 = min(tid * per, A.n_seqs), s1 = min(s0 + per, A.n_seqs);
-    int64_t mine = 0;
-    int begin;
-    for (int s = s0; s < s1; ++s) mine += read(s, begin).units_per_head() * A.Hkv;
+    int64_t mine = 0, per_head = 0;
+    int begin = 0;
+    SeqWork<kShift> w;
+    for (int s = s0; s < s1; ++s) {
+        read(s, w, begin);
+        per_head = w.units_per_head();
+        mine += per_head * A.Hkv;
+    }
     int64_t upto = mine;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
@@ -79,25 +76,26 @@ __device__ __forceinline__ void paged_find_run(const PagedArgs& A, int64_t* scra
         total += scratch[i];
     }
     const int64_t ctas = min(static_cast<int64_t>(gridDim.x), total), c = blockIdx.x;
-    if (c < ctas) {
-        int64_t off = paged_first_unit(total, ctas, c) - before;
+    if (c < ctas && mine > 0) {
+        const PagedShares shares(total, ctas);
+        int64_t off = shares.first(c) - before;
         if (off >= 0 && off < mine) {
-            for (int s = s0; s < s1; ++s) {
-                const SeqWork w = read(s, begin);
-                const int64_t units = w.units_per_head() * A.Hkv;
-                if (off < units) {
-                    paged_begin_run(w, s, off, total, ctas, c, run);
-                    break;
-                }
-                off -= units;
+            int s = s0;
+            for (; per > 1 && s < s1; ++s) {          // with one sequence a thread it is at hand
+                read(s, w, begin);
+                per_head = w.units_per_head();
+                if (off < per_head * A.Hkv) break;
+                off -= per_head * A.Hkv;
             }
+            paged_begin_run(w, s, begin, per_head, off, shares, c, run);
         }
     }
     __syncthreads();
 }
 
 // Keys that token i of the segment's tile sees
-__device__ __forceinline__ int paged_limit(const PagedSegment& g, int i)
+template <int kShift>
+__device__ __forceinline__ int paged_limit(const PagedSegment<kShift>& g, int i)
 {
     return g.w.causal ? max(0, min(g.w.len, g.base + i + 1)) : g.w.len;
 }

@@ -10,31 +10,52 @@ from paper_2609_09721_b200 import build
 
 HARNESS = r"""
 #include "paged_units.h"
+template <int kShift>
 struct Reader {
     const int32_t *cu, *lens;
-    int step, keys, causal;
-    efq::SeqWork operator()(int s, int& begin) const { begin = cu[s]; return {cu[s + 1] - cu[s], lens[s], step, keys, causal, 0}; }
+    int step, causal;
+    void operator()(int s, efq::SeqWork<kShift>& w, int& begin) const { begin = cu[s]; w.set(cu[s + 1] - cu[s], lens[s], step, causal); }
 };
-extern "C" int64_t before(int lq, int len, int step, int keys, int causal, int n) { return efq::SeqWork{lq, len, step, keys, causal, 0}.units_before(n); }
-extern "C" int tile_of(int lq, int len, int step, int keys, int causal, int64_t off) { return efq::SeqWork{lq, len, step, keys, causal, 0}.tile_of(off); }
-// segments of all CTAs: (cta, begins, seq, head, token0, tokens, base, j0, j1, n) each; the number of them, -1 if there are more than fit
-extern "C" int64_t segments(const int32_t* cu, const int32_t* lens, int n_seqs, int heads, int step, int keys, int causal, int grid, int32_t* out, int64_t most)
+template <int kShift>
+efq::SeqWork<kShift> work(int lq, int len, int step, int causal)
 {
-    const Reader read{cu, lens, step, keys, causal};
+    efq::SeqWork<kShift> w;
+    w.set(lq, len, step, causal);
+    return w;
+}
+extern "C" int64_t before(int lq, int len, int step, int keys, int causal, int n)
+{
+    return keys == 64 ? work<6>(lq, len, step, causal).units_before(n) : work<7>(lq, len, step, causal).units_before(n);
+}
+extern "C" int tile_of(int lq, int len, int step, int keys, int causal, int64_t off)
+{
+    return keys == 64 ? work<6>(lq, len, step, causal).tile_of(off) : work<7>(lq, len, step, causal).tile_of(off);
+}
+template <int kShift>
+int64_t all_segments(const int32_t* cu, const int32_t* lens, int n_seqs, int heads, int step, int causal, int grid, int32_t* out, int64_t most)
+{
+    const Reader<kShift> read{cu, lens, step, causal};
+    efq::SeqWork<kShift> w;
     int64_t total = 0, n = 0;
     int b;
-    for (int s = 0; s < n_seqs; ++s) total += read(s, b).units_per_head() * heads;
+    for (int s = 0; s < n_seqs; ++s) {
+        read(s, w, b);
+        total += w.units_per_head() * heads;
+    }
     const int64_t ctas = grid < total ? grid : total;
+    if (total == 0) return 0;
+    const efq::PagedShares shares(total, ctas);
     for (int64_t c = 0; c < ctas; ++c) {
-        efq::PagedRun run{};
-        int64_t off = efq::paged_first_unit(total, ctas, c);
+        efq::PagedRun<kShift> run{};
+        int64_t off = shares.first(c);
         for (int s = 0; s < n_seqs; ++s) {
-            const efq::SeqWork w = read(s, b);
-            if (off < w.units_per_head() * heads) { efq::paged_begin_run(w, s, off, total, ctas, c, &run); break; }
-            off -= w.units_per_head() * heads;
+            read(s, w, b);
+            const int64_t per_head = w.units_per_head();
+            if (off < per_head * heads) { efq::paged_begin_run(w, s, b, per_head, off, shares, c, &run); break; }
+            off -= per_head * heads;
         }
-        efq::PagedWalk<Reader> walk(read, n_seqs, heads, run);
-        efq::PagedSegment g;
+        efq::PagedWalk<kShift, Reader<kShift>> walk(read, n_seqs, heads, run);
+        efq::PagedSegment<kShift> g;
         for (bool first = true; walk.next(g); first = false) {
             if (n == most) return -1;
             const int32_t v[10] = {(int32_t)c, first ? run.begins : (int32_t)c, g.seq, g.head, g.token0, g.tokens, g.base, g.j0, g.j1, g.n};
@@ -43,6 +64,12 @@ extern "C" int64_t segments(const int32_t* cu, const int32_t* lens, int n_seqs, 
         }
     }
     return n;
+}
+// segments of all CTAs: (cta, begins, seq, head, token0, tokens, base, j0, j1, n) each; the number of them, -1 if there are more than fit
+extern "C" int64_t segments(const int32_t* cu, const int32_t* lens, int n_seqs, int heads, int step, int keys, int causal, int grid, int32_t* out, int64_t most)
+{
+    return keys == 64 ? all_segments<6>(cu, lens, n_seqs, heads, step, causal, grid, out, most)
+                      : all_segments<7>(cu, lens, n_seqs, heads, step, causal, grid, out, most);
 }
 """
 
