@@ -13,55 +13,118 @@ namespace {
 
 constexpr int kMaxCtas = 256;            // of the first kernel; the workspace has room for the parts of as many
 
-// Joins the parts of the query tiles that span CTAs.  blockIdx.x: the CTA that ended the tile.  kWarps warps take a row, every kWarps-th
-// part each, a lane four channels.  Few rows may have a part from every CTA (one long context), many rows have two or three as a rule.
-// half_rows: rows of the first of the two halves of a tile of many rows (whole tokens); parts keep kRows / 2 for each half.
-template <typename T, int kRows, int kWarps>
-__global__ void __launch_bounds__(128) paged_join_kernel(const __grid_constant__ PagedArgs A, int half_rows)
+// Joins the parts of the query tiles that span CTAs.  blockIdx.x: the CTA that ended the tile, blockIdx.y: a row of it (and further ones where
+// a tile has more).  Four warps take every fourth part each, four of them at a time, a lane four channels: bound by latency, so maxima, sums
+// and outputs of as many parts are asked for at once.  One long context may leave a part in every CTA.
+template <typename T, int kRows>
+__global__ void __launch_bounds__(128) paged_join_kernel(const __grid_constant__ PagedArgs A)
 {
-    constexpr int kAtOnce = 4 / kWarps;         // rows of a block
+    constexpr int kWarps = 4, kAhead = 4;
     ptx::grid_wait();
-    const int c = blockIdx.x, lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) % kWarps, which = (threadIdx.x >> 5) / kWarps;
-    const PagedRecord rec = {__ldcg(&A.records[c].first), __ldcg(&A.records[c].token0), __ldcg(&A.records[c].tokens), __ldcg(&A.records[c].head)};
+    const int c = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int4 found = __ldcg(reinterpret_cast<const int4*>(A.records + c));
+    const PagedRecord rec = {found.x, found.y, found.z, found.w};
     if (rec.first < 0) return;
-    __shared__ float4 xs[4][32];
-    __shared__ float ls[4];
-    for (int r = blockIdx.y * kAtOnce + which; r < rec.tokens * A.G; r += gridDim.y * kAtOnce) {
-        const int at = r < half_rows ? r : kRows / 2 + r - half_rows;
-        auto slot = [&](int i) { return (2 * i + (i == rec.first ? 1 : 0)) * kRows + at; };
-        float top = -INFINITY;
-        for (int i = rec.first + lane; i <= c; i += 32) top = fmaxf(top, __ldcg(&A.part_ml[slot(i)].x));
-#pragma unroll
-        for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-        const float base = top == -INFINITY ? 0.0f : top;
+    for (int r = blockIdx.y; r < rec.tokens * A.G; r += gridDim.y) {
+        float top = -INFINITY, l = 0.0f;
         float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        float l = 0.0f;
-#pragma unroll 4
-        for (int i = rec.first + warp; i <= c; i += kWarps) {
-            const float2 ml = __ldcg(&A.part_ml[slot(i)]);
-            const float4 y = __ldcg(reinterpret_cast<const float4*>(A.part_o + static_cast<int64_t>(slot(i)) * kPagedD) + lane);
-            const float f = paged_exp2(ml.x - base);
-            l = fmaf(ml.y, f, l);
+        for (int first = rec.first + warp; first <= c; first += kAhead * kWarps) {
+            float2 ml[kAhead];
+            float4 y[kAhead];
+            float upto = top;
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int i = first + u * kWarps;
+                const int64_t slot = (2 * i + (i == rec.first ? 1 : 0)) * kRows + r;
+                ml[u] = make_float2(-INFINITY, 0.0f);
+                y[u] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (i <= c) {
+                    ml[u] = __ldcg(A.part_ml + slot);
+                    y[u] = __ldcg(reinterpret_cast<const float4*>(A.part_o + slot * kPagedD) + lane);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) upto = fmaxf(upto, ml[u].x);
+            const float base = upto == -INFINITY ? 0.0f : upto, before = paged_exp2(top - base);
+            top = upto;
+            l *= before;
+            x.x *= before; x.y *= before; x.z *= before; x.w *= before;
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const float f = paged_exp2(ml[u].x - base);
+                l = fmaf(ml[u].y, f, l);
+                x.x = fmaf(y[u].x, f, x.x); x.y = fmaf(y[u].y, f, x.y); x.z = fmaf(y[u].z, f, x.z); x.w = fmaf(y[u].w, f, x.w);
+            }
+        }
+        __shared__ float4 xs[kWarps][32];
+        __shared__ float2 mls[kWarps];
+        xs[warp][lane] = x;
+        if (lane == 0) mls[warp] = make_float2(top, l);
+        __syncthreads();
+        top = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) top = fmaxf(top, mls[w].x);
+        const float base = top == -INFINITY ? 0.0f : top;
+        x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        l = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            const float4 y = xs[w][lane];
+            const float f = paged_exp2(mls[w].x - base);
+            l = fmaf(mls[w].y, f, l);
             x.x = fmaf(y.x, f, x.x); x.y = fmaf(y.y, f, x.y); x.z = fmaf(y.z, f, x.z); x.w = fmaf(y.w, f, x.w);
         }
-        if (kWarps > 1) {
-            xs[warp][lane] = x;
-            if (lane == 0) ls[warp] = l;
-            __syncthreads();
-#pragma unroll
-            for (int w = 1; w < kWarps; ++w) {
-                const float4 y = xs[w][lane];
-                x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
-                l += ls[w];
-            }
-            __syncthreads();
-        }
+        __syncthreads();
         if (warp != 0) continue;
         const int token = rec.token0 + r / A.G, head = rec.head * A.G + r % A.G;
         const float inv = l == 0.0f ? 0.0f : 1.0f / l;
         *reinterpret_cast<uint2*>(A.o + token * A.o_token + head * A.o_head + 8 * lane) =
             make_uint2(Pack2<T>::round(x.x * inv, x.y * inv), Pack2<T>::round(x.z * inv, x.w * inv));
         if (A.lse != nullptr && lane == 0) A.lse[static_cast<int64_t>(token) * (A.Hkv * A.G) + head] = top * kLn2 + logf(l);
+    }
+}
+
+// The same for the parts of the kernel for many rows: [half][group of four channels][row].  blockIdx.y: 32 rows of a half; a lane takes a row
+// and a warp every fourth group of channels, so that loads are whole lines, and the rows leave by way of shared memory as whole lines too.
+template <typename T>
+__global__ void __launch_bounds__(128) paged_join_chunk_kernel(const __grid_constant__ PagedArgs A)
+{
+    constexpr int kGroups = kPagedD / 4 / 4;        // of a warp
+    __shared__ uint2 rows[32][kPagedD / 4 + 1];
+    ptx::grid_wait();
+    const int c = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, half = blockIdx.y >> 2, r = (blockIdx.y & 3) * 32 + lane;
+    const int4 found = __ldcg(reinterpret_cast<const int4*>(A.records + c));
+    const PagedRecord rec = {found.x, found.y, found.z, found.w};
+    const int per = A.step >> 1, tokens = max(0, min(per, rec.tokens - half * per)), first_row = (blockIdx.y & 3) * 32;
+    if (rec.first < 0 || first_row >= tokens * A.G) return;
+    float top = -INFINITY, l = 0.0f;
+    float4 x[kGroups];
+#pragma unroll
+    for (int u = 0; u < kGroups; ++u) x[u] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int i = rec.first; i <= c; ++i) {
+        const int64_t at = (2 * i + (i == rec.first ? 1 : 0)) * 2 + half;
+        const float2 ml = __ldcg(A.part_ml + at * kChunkRows + r);
+        const float4* const part = reinterpret_cast<const float4*>(A.part_o + at * kChunkRows * kPagedD) + r;
+        float4 y[kGroups];
+#pragma unroll
+        for (int u = 0; u < kGroups; ++u) y[u] = __ldcg(part + (4 * u + warp) * kChunkRows);
+        const float upto = fmaxf(top, ml.x), base = upto == -INFINITY ? 0.0f : upto, before = paged_exp2(top - base), f = paged_exp2(ml.x - base);
+        top = upto;
+        l = l * before + ml.y * f;
+#pragma unroll
+        for (int u = 0; u < kGroups; ++u)
+            x[u] = make_float4(x[u].x * before + y[u].x * f, x[u].y * before + y[u].y * f, x[u].z * before + y[u].z * f, x[u].w * before + y[u].w * f);
+    }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+    for (int u = 0; u < kGroups; ++u)
+        rows[lane][4 * u + warp] = make_uint2(Pack2<T>::round(x[u].x * inv, x[u].y * inv), Pack2<T>::round(x[u].z * inv, x[u].w * inv));
+    if (A.lse != nullptr && warp == 0 && r < tokens * A.G)
+        A.lse[static_cast<int64_t>(rec.token0 + half * per + r / A.G) * (A.Hkv * A.G) + rec.head * A.G + r % A.G] = top * kLn2 + logf(l);
+    __syncthreads();
+    for (int i = warp; i < 32 && first_row + i < tokens * A.G; i += 4) {
+        const int row = first_row + i, token = rec.token0 + half * per + row / A.G, head = rec.head * A.G + row % A.G;
+        *reinterpret_cast<uint2*>(A.o + token * A.o_token + head * A.o_head + 8 * lane) = rows[i][lane];
     }
 }
 
@@ -100,7 +163,7 @@ PagedPlan plan_paged(int64_t group_rows)
     p.rows = group_rows <= 16 ? 16 : group_rows <= 32 ? 32 : 2 * kChunkRows;
     p.ml = static_cast<size_t>(2 * kMaxCtas) * p.rows * kPagedD * 4;
     p.records = p.ml + static_cast<size_t>(2 * kMaxCtas) * p.rows * sizeof(float2);
-    p.total = p.records + kMaxCtas * sizeof(PagedRecord);
+    p.total = p.records + kMaxCtas * sizeof(PagedRecord);       // records on 16 bytes: 2 * kMaxCtas * rows is a multiple of 8
     return p;
 }
 
@@ -121,7 +184,7 @@ cudaError_t launch_few_rows(const CUtensorMap& mq, const CUtensorMap& mk, const 
     constexpr int smem = static_cast<int>(sizeof(FewSmem<kM>)) + 1024;
     cudaError_t e = allow_smem(paged_few_kernel<T, kM>, smem, done, dev);
     if (e == cudaSuccess) e = launch_overlapped(paged_few_kernel<T, kM>, dim3(static_cast<unsigned>(ctas)), kFewThreads, smem, st, mq, mk, mv, A);
-    if (e == cudaSuccess) e = launch_overlapped(paged_join_kernel<T, 16 * kM, 4>, dim3(static_cast<unsigned>(ctas), static_cast<unsigned>(max_rows)), 128, 0, st, A, 16 * kM);
+    if (e == cudaSuccess) e = launch_overlapped(paged_join_kernel<T, 16 * kM>, dim3(static_cast<unsigned>(ctas), static_cast<unsigned>(max_rows)), 128, 0, st, A);
     return e;
 }
 
@@ -132,7 +195,7 @@ cudaError_t launch_chunk(const CUtensorMap& mq, const CUtensorMap& mk, const CUt
     constexpr int smem = static_cast<int>(sizeof(ChunkSmem)) + 1024;
     cudaError_t e = allow_smem(paged_chunk_kernel<T>, smem, done, dev);
     if (e == cudaSuccess) e = launch_overlapped(paged_chunk_kernel<T>, dim3(static_cast<unsigned>(ctas)), kChunkThreads, smem, st, mq, mk, mv, A);
-    if (e == cudaSuccess) e = launch_overlapped(paged_join_kernel<T, 2 * kChunkRows, 1>, dim3(static_cast<unsigned>(ctas), 16), 128, 0, st, A, A.step / 2 * A.G);
+    if (e == cudaSuccess) e = launch_overlapped(paged_join_chunk_kernel<T>, dim3(static_cast<unsigned>(ctas), 2 * kChunkRows / 32), 128, 0, st, A);
     return e;
 }
 
@@ -179,6 +242,7 @@ efq_status_t paged_attention(const efq_rows_t* q, float* lse, int64_t total, int
     A.o = static_cast<char*>(q->dst);
     A.o_token = 2 * q->dst_token;
     A.o_head = 2 * q->dst_head;
+    A.o_wide = ((reinterpret_cast<uintptr_t>(A.o) | static_cast<uintptr_t>(A.o_token) | static_cast<uintptr_t>(A.o_head)) & 31u) == 0 ? 1 : 0;
     A.lse = lse;
     char* const ws = static_cast<char*>(workspace);
     A.part_o = reinterpret_cast<float*>(ws);
@@ -200,7 +264,7 @@ efq_status_t paged_attention(const efq_rows_t* q, float* lse, int64_t total, int
         !encode_rows(&mv, dtype, cache->v, 4, dims, v_strides, box))
         return EFQ_ERR_CUDA;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const int max_rows = A.step * G;
+    const int max_rows = group_rows < A.step * G ? static_cast<int>(group_rows) : A.step * G;       // the join's blocks; with more rows they go round
     using Bf = __nv_bfloat16;
     const bool bf = dtype == EFQ_BF16;
     const cudaError_t e = many ? (bf ? launch_chunk<Bf>(mq, mk, mv, A, ctas, dev, s) : launch_chunk<__half>(mq, mk, mv, A, ctas, dev, s))

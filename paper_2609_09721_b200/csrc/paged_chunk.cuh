@@ -16,6 +16,7 @@
 
 namespace efq {
 
+constexpr int kChunkItem = 2;                                  // what a query tile costs beside its key tiles, in key tiles
 constexpr int kChunkShift = 7, kChunkKeys = 1 << kChunkShift, kChunkRows = 128;      // keys of a tile, rows of a half
 constexpr int kChunkThreads = 384;
 constexpr int kChunkSlots = 5;
@@ -28,7 +29,7 @@ struct __align__(1024) ChunkSmem {
     uint8_t kv[kChunkSlots][2][kChunkPart];
     uint64_t full[kChunkSlots], empty[kChunkSlots], q_full, q_empty, s_full[2], p_ready[2], p_rest[2], o_full[2], v_tail, v_clean, turn[2], drained[2];
     int64_t scratch[kChunkThreads / 32];
-    PagedRun<kChunkShift> run;
+    PagedRun<kChunkShift, kChunkItem> run;
     uint32_t tmem_base;
     volatile uint32_t failed;
 };
@@ -88,6 +89,13 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
                  "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr) : "memory");
 }
 
+// 32 bytes, a whole sector; p on 32 bytes
+__device__ __forceinline__ void store8(void* p, const uint32_t (&u)[8])
+{
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"l"(p), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]) : "memory");
+}
+
 // Tells the compiler that a value is the same in all lanes.
 template <typename V>
 __device__ __forceinline__ V uniform(V x) { return __shfl_sync(0xffffffffu, x, 0); }
@@ -96,7 +104,7 @@ __device__ __forceinline__ V uniform(V x) { return __shfl_sync(0xffffffffu, x, 0
 struct ChunkHalf {
     int tokens, end;
 };
-__device__ __forceinline__ ChunkHalf chunk_half(const PagedSegment<kChunkShift>& g, int half, int step)
+__device__ __forceinline__ ChunkHalf chunk_half(const PagedSegment<kChunkShift, kChunkItem>& g, int half, int step)
 {
     const int per = step >> 1;
     ChunkHalf h;
@@ -141,11 +149,11 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
     ptx::tc_fence_before_sync();
     ptx::grid_wait();
     ptx::grid_launch_next();
-    paged_find_run<kChunkThreads, kChunkShift>(A, sm->scratch, &sm->run);      // two barriers of the block
+    paged_find_run<kChunkThreads, kChunkShift, kChunkItem>(A, sm->scratch, &sm->run);      // barriers of the block
     ptx::tc_fence_after_sync();
     const uint32_t tmem = sm->tmem_base;
-    PagedWalk<kChunkShift, PagedReader<kChunkShift>> walk(PagedReader<kChunkShift>{A}, A.n_seqs, A.Hkv, sm->run);
-    PagedSegment<kChunkShift> g;
+    PagedWalk<kChunkShift, kChunkItem, PagedReader<kChunkShift, kChunkItem>> walk(PagedReader<kChunkShift, kChunkItem>{A}, A.n_seqs, A.Hkv, sm->run);
+    PagedSegment<kChunkShift, kChunkItem> g;
 
     if (warp >= 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kChunkRegsLess));
@@ -469,7 +477,8 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
             const int token = g.token0 + i, head = g.head * A.G + r % A.G, slot = 2 * blockIdx.x + (g.j0 == 0 ? 1 : 0);
             const float inv = l == 0.0f ? 0.0f : 1.0f / l;
             char* const dst = A.o + token * A.o_token + head * A.o_head;
-            float4* const part = reinterpret_cast<float4*>(A.part_o + (static_cast<int64_t>(slot) * 2 * kChunkRows + w * kChunkRows + r) * kPagedD);
+            // of four channels the 128 rows side by side, so that a warp's stores are whole lines
+            float4* const part = reinterpret_cast<float4*>(A.part_o + (static_cast<int64_t>(slot) * 2 + w) * kChunkRows * kPagedD) + r;
 #pragma unroll 1
             for (int q = 0; q < 4; ++q) {
                 float o[32];
@@ -482,12 +491,21 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
                 }
                 if (mine && all) {
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
-                        reinterpret_cast<uint4*>(dst)[4 * q + c] = make_uint4(Pack2<T>::round(o[8 * c] * inv, o[8 * c + 1] * inv), Pack2<T>::round(o[8 * c + 2] * inv, o[8 * c + 3] * inv),
-                                                                             Pack2<T>::round(o[8 * c + 4] * inv, o[8 * c + 5] * inv), Pack2<T>::round(o[8 * c + 6] * inv, o[8 * c + 7] * inv));
+                    for (int c = 0; c < 2; ++c) {
+                        uint32_t u[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) u[i] = Pack2<T>::round(o[16 * c + 2 * i] * inv, o[16 * c + 2 * i + 1] * inv);
+                        char* const at = dst + 64 * q + 32 * c;
+                        if (A.o_wide) {
+                            store8(at, u);
+                        } else {
+                            reinterpret_cast<uint4*>(at)[0] = make_uint4(u[0], u[1], u[2], u[3]);
+                            reinterpret_cast<uint4*>(at)[1] = make_uint4(u[4], u[5], u[6], u[7]);
+                        }
+                    }
                 } else if (mine) {
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) part[8 * q + c] = make_float4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
+                    for (int c = 0; c < 8; ++c) part[(8 * q + c) * kChunkRows] = make_float4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
                 }
             }
             ptx::tc_fence_before_sync();

@@ -13,6 +13,7 @@
 
 namespace efq {
 
+constexpr int kFewItem = 1;                     // what a query tile costs beside its key tiles, in key tiles
 constexpr int kFewShift = 6, kFewKeys = 1 << kFewShift;       // of a stage
 constexpr int kFewWarps = 8;                    // that compute
 constexpr int kFewThreads = (kFewWarps + 1) * 32;
@@ -32,7 +33,7 @@ struct __align__(1024) FewSmem {
     float2 row_ml[16 * kM];
     uint64_t full[kStages], empty[kStages], q_full[2], q_empty[2];
     int64_t scratch[64];
-    PagedRun<kFewShift> run;
+    PagedRun<kFewShift, kFewItem> run;
     uint32_t bad[kStages];                      // the tile lies on an entry that is no page
     volatile uint32_t failed;
 };
@@ -94,7 +95,7 @@ __device__ __forceinline__ void few_bar() { asm volatile("bar.sync 1, 256;" ::: 
 
 // Loads of one tile: lane i takes the i-th page of it.  `entry`: that page's entry in the table (below zero where it is none).
 template <int kStages, typename Smem>
-__device__ __forceinline__ void few_load_tile(Smem* sm, int stage, const CUtensorMap& mk, const CUtensorMap& mv, const PagedArgs& A, const PagedSegment<kFewShift>& g,
+__device__ __forceinline__ void few_load_tile(Smem* sm, int stage, const CUtensorMap& mk, const CUtensorMap& mv, const PagedArgs& A, const PagedSegment<kFewShift, kFewItem>& g,
                                               int j, int entry, int lane)
 {
     const int P = 1 << A.page_shift, box = min(P, kFewKeys), key = j * kFewKeys + lane * box;
@@ -142,9 +143,9 @@ paged_few_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
     }
     ptx::grid_wait();
     ptx::grid_launch_next();
-    paged_find_run<kFewThreads, kFewShift>(A, sm->scratch, &sm->run);      // two barriers of the block
-    PagedWalk<kFewShift, PagedReader<kFewShift>> walk(PagedReader<kFewShift>{A}, A.n_seqs, A.Hkv, sm->run);
-    PagedSegment<kFewShift> g;
+    paged_find_run<kFewThreads, kFewShift, kFewItem>(A, sm->scratch, &sm->run);      // barriers of the block
+    PagedWalk<kFewShift, kFewItem, PagedReader<kFewShift, kFewItem>> walk(PagedReader<kFewShift, kFewItem>{A}, A.n_seqs, A.Hkv, sm->run);
+    PagedSegment<kFewShift, kFewItem> g;
 
     if (warp == kFewWarps) {
         // ------------------------------------------------------------ loads

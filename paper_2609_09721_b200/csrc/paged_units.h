@@ -12,35 +12,35 @@
 
 #ifdef __CUDACC__
 #define EFQ_HD __host__ __device__ __forceinline__
-#define EFQ_HD_CALLED __host__ __device__ __noinline__      // once a CTA: kept out of the way of the loops' code
 #else
 #define EFQ_HD inline
-#define EFQ_HD_CALLED inline
 #endif
 
 namespace efq {
 
-// sum over i < n of floor((a i + b) / m); a, b >= 0.  The lattice points below a line, by Euclid's algorithm on (m, a).
-EFQ_HD_CALLED int64_t floor_sum(uint64_t n, uint64_t m, uint64_t a, uint64_t b)
+// sum over i < n of floor((b + a i) / 2^shift), a > 0, b >= 0.  The terms grow by a fixed amount from one period of
+// 2^shift / gcd(a, 2^shift) terms to the next, so two partial periods are summed term by term and the rest is arithmetic.
+EFQ_HD int64_t paged_floor_sum(int64_t n, int shift, uint32_t a, uint32_t b)
 {
-    uint64_t sum = 0;
-    while (n > 0) {
-        sum += n * (n - 1) / 2 * (a / m) + n * (b / m);
-        a %= m;
-        b %= m;
-        const uint64_t top = a * n + b;
-        if (top < m) break;
-        n = top / m;
-        b = top % m;
-        const uint64_t t = m;
-        m = a;
-        a = t;
+    int low = 0;
+    while (low < shift && ((a >> low) & 1u) == 0u) ++low;
+    const int period_log = shift - low;
+    const uint32_t period = 1u << period_log;
+    const int64_t full = n >> period_log, grows = static_cast<int64_t>(a) >> low;         // period * a / 2^shift
+    const uint32_t rest = static_cast<uint32_t>(n - (full << period_log)), upto = full > 0 ? period : rest;
+    int64_t of_period = 0, of_rest = 0;
+    uint64_t x = b;
+    for (uint32_t i = 0; i < upto; ++i, x += a) {
+        if (i == rest) of_rest = of_period;
+        of_period += static_cast<int64_t>(x >> shift);
     }
-    return static_cast<int64_t>(sum);
+    if (rest == upto) of_rest = of_period;
+    return full * of_period + grows * static_cast<int64_t>(period) * (full * (full - 1) / 2) + static_cast<int64_t>(rest) * full * grows + of_rest;
 }
 
-// One sequence of the step: lq new tokens in query tiles of `step` tokens, len keys in tiles of 2^kShift.
-template <int kShift>
+// One sequence of the step: lq new tokens in query tiles of `step` tokens, len keys in tiles of 2^kShift.  A query tile costs its key tiles and
+// kItem more (its queries' load, its output): so many units of it stand for no key tile.
+template <int kShift, int kItem>
 struct SeqWork {
     static constexpr int kKeys = 1 << kShift;
     int32_t lq, len, step, tiles;
@@ -63,52 +63,42 @@ struct SeqWork {
         const int n = len - lq + (i + 1) * step;
         return n < 0 ? 0 : n;
     }
-    // a tile that sees nothing is a unit too: its rows have to be written
-    EFQ_HD int units(int i) const
+    // one that sees nothing has a key tile all the same: its rows have to be written
+    EFQ_HD int key_tiles(int i) const
     {
         const int n = static_cast<int>((static_cast<uint32_t>(limit(i)) + (kKeys - 1u)) >> kShift);
         return n > 0 ? n : 1;
     }
+    EFQ_HD int units(int i) const { return key_tiles(i) + kItem; }
     // units of the first n tiles
     EFQ_HD int64_t units_before(int n) const
     {
         if (n <= 0) return 0;
         if (!causal || tiles == 1) return static_cast<int64_t>(n) * units(0);
-        const int64_t base = static_cast<int64_t>(len) - lq;
-        const int64_t blind = base >= 0 ? 0 : -base / step;                     // tiles that see nothing
+        const int base = len - lq;
+        const int blind = base >= 0 ? 0 : -base / step;                         // tiles that see nothing
         const int full = n < tiles ? n : tiles - 1;                             // the last one ends at len and not at a multiple of step
-        int64_t sum = blind < full ? blind : full;
+        int64_t sum = (blind < full ? blind : full) + static_cast<int64_t>(n) * kItem;
         if (full > blind)
-            sum += floor_sum(static_cast<uint64_t>(full - blind), static_cast<uint64_t>(kKeys), static_cast<uint64_t>(step),
-                             static_cast<uint64_t>(base + (blind + 1) * step + kKeys - 1));
-        return n == tiles ? sum + units(tiles - 1) : sum;
+            sum += paged_floor_sum(full - blind, kShift, static_cast<uint32_t>(step),
+                                   static_cast<uint32_t>(static_cast<int64_t>(base) + static_cast<int64_t>(blind + 1) * step + kKeys - 1));
+        return n == tiles ? sum + key_tiles(tiles - 1) : sum;
     }
     EFQ_HD int64_t units_per_head() const { return units_before(tiles); }
-    // the tile that holds unit `off` of a head
-    EFQ_HD int tile_of(int64_t off) const
-    {
-        int lo = 0, hi = tiles;
-        while (hi - lo > 1) {
-            const int mid = lo + (hi - lo) / 2;
-            if (units_before(mid) <= off) lo = mid;
-            else hi = mid;
-        }
-        return lo;
-    }
 };
 
 // The run of units of one CTA, and a walk along it.  Every role of a kernel walks by itself.
-template <int kShift>
+template <int kShift, int kItem>
 struct PagedRun {
-    int64_t left;                       // units
+    int64_t left, off;                  // units; the first one's place in its head
     int32_t seq, begin, head, tile, unit;       // where it begins; the sequence's first token in the step
     int32_t begins;                     // CTA that holds unit 0 of that query tile
-    SeqWork<kShift> w;                  // of that sequence
+    SeqWork<kShift, kItem> w;           // of that sequence
 };
 
-template <int kShift>
+template <int kShift, int kItem>
 struct PagedSegment {
-    SeqWork<kShift> w;
+    SeqWork<kShift, kItem> w;
     int32_t seq, head, token0, tokens;              // tokens of the step: token0 .. token0 + tokens - 1
     int32_t base;                                   // token i of the tile sees base + i + 1 keys (causal), all len otherwise
     int32_t j0, j1, n;                              // key tiles of the run, of the query tile
@@ -132,65 +122,82 @@ struct PagedShares {
         return static_cast<int64_t>(unit < wide ? paged_divide(unit, each + 1) : more + paged_divide(unit - wide, each));
     }
 };
-// The run of CTA c, which begins at unit `off` of sequence s.
-template <int kShift>
-EFQ_HD void paged_begin_run(const SeqWork<kShift>& w, int s, int begin, int64_t per_head, int64_t off, const PagedShares& shares, int64_t c, PagedRun<kShift>* run)
+// The run of CTA c, which begins at unit `off` of sequence s; paged_begin_tile() has to follow with the query tile that holds unit run->unit of
+// the head.
+template <int kShift, int kItem>
+EFQ_HD void paged_begin_run(const SeqWork<kShift, kItem>& w, int s, int begin, int64_t per_head, int64_t off, const PagedShares& shares, int64_t c,
+                            PagedRun<kShift, kItem>* run)
 {
     run->left = shares.units(c);
     run->seq = s;
     run->begin = begin;
     run->w = w;
     run->head = static_cast<int32_t>(paged_divide(off, per_head));
-    off -= run->head * per_head;
-    run->tile = w.tile_of(off);
-    run->unit = static_cast<int32_t>(off - w.units_before(run->tile));
-    run->begins = static_cast<int32_t>(shares.cta_of(shares.first(c) - run->unit));
+    run->off = off - run->head * per_head;
+    run->tile = 0;
+    run->unit = 0;
+    run->begins = static_cast<int32_t>(c);
+}
+// Whether query tile `tile` holds the run's first unit; if so, the run begins there.
+template <int kShift, int kItem>
+EFQ_HD bool paged_begin_tile(int tile, const PagedShares& shares, int64_t c, PagedRun<kShift, kItem>* run)
+{
+    const int64_t unit = run->off - run->w.units_before(tile);
+    if (unit < 0 || unit >= run->w.units(tile)) return false;
+    run->tile = tile;
+    run->unit = static_cast<int32_t>(unit);
+    run->begins = static_cast<int32_t>(shares.cta_of(shares.first(c) - unit));
+    return true;
 }
 
 // `Read`: sequence s of the step and its first token there.
-template <int kShift, typename Read>
+template <int kShift, int kItem, typename Read>
 struct PagedWalk {
     Read read;
     int n_seqs, heads;
     int64_t left;
     int seq, head, tile, unit, begin;
-    SeqWork<kShift> w;
+    SeqWork<kShift, kItem> w;
 
-    EFQ_HD PagedWalk(Read r, int n, int h, const PagedRun<kShift>& run)
+    EFQ_HD PagedWalk(Read r, int n, int h, const PagedRun<kShift, kItem>& run)
         : read(r), n_seqs(n), heads(h), left(run.left), seq(run.seq), head(run.head), tile(run.tile), unit(run.unit), begin(run.begin), w(run.w)
     {
     }
     // the next segment of the run; false at its end
-    EFQ_HD bool next(PagedSegment<kShift>& g)
+    EFQ_HD bool next(PagedSegment<kShift, kItem>& g)
     {
-        if (left <= 0) return false;
-        if (tile == w.tiles) {
-            tile = 0;
-            if (++head == heads) {
-                head = 0;
-                do {
-                    if (++seq >= n_seqs) {          // tables that changed under way
-                        left = 0;
-                        return false;
-                    }
-                    read(seq, w, begin);
-                } while (w.lq == 0);
+        while (left > 0) {
+            if (tile == w.tiles) {
+                tile = 0;
+                if (++head == heads) {
+                    head = 0;
+                    do {
+                        if (++seq >= n_seqs) {          // tables that changed under way
+                            left = 0;
+                            return false;
+                        }
+                        read(seq, w, begin);
+                    } while (w.lq == 0);
+                }
             }
+            const int first = tile * w.step, n = w.key_tiles(tile), from = unit, all = n + kItem - from;
+            const int taken = all < left ? all : static_cast<int>(left);
+            left -= taken;
+            unit = 0;
+            ++tile;
+            if (from >= n) continue;                    // only what stands for no key tile
+            g.w = w;
+            g.seq = seq;
+            g.head = head;
+            g.token0 = begin + first;
+            g.tokens = w.lq - first < w.step ? w.lq - first : w.step;
+            g.base = w.len - w.lq + first;
+            g.n = n;
+            g.j0 = from;
+            g.j1 = from + taken < n ? from + taken : n;
+            return true;
         }
-        const int first = tile * w.step, n = w.units(tile);
-        g.w = w;
-        g.seq = seq;
-        g.head = head;
-        g.token0 = begin + first;
-        g.tokens = w.lq - first < w.step ? w.lq - first : w.step;
-        g.base = w.len - w.lq + first;
-        g.n = n;
-        g.j0 = unit;
-        g.j1 = n - unit < left ? n : static_cast<int>(unit + left);
-        left -= g.j1 - g.j0;
-        unit = 0;
-        ++tile;
-        return true;
+        return false;
     }
 };
 

@@ -7,6 +7,12 @@
 
 namespace efq {
 
+// Of a CTA that ends a query tile which an earlier one began: where its parts and its rows are.
+struct __align__(16) PagedRecord {
+    int32_t first;                      // CTA that began it; -1: nothing to join
+    int32_t token0, tokens, head;
+};
+
 // What the kernels get; the tables are device memory.
 struct PagedArgs {
     const int32_t *page_table, *cu_seqlens, *seq_lens;
@@ -17,24 +23,19 @@ struct PagedArgs {
     float scale_log2;                   // softmax scale / ln 2
     char* o;
     int64_t o_token, o_head;            // bytes
+    int32_t o_wide;                     // rows of o lie on 32 bytes
     float* lse;                         // [total, Hkv * G]
     float* part_o;
     float2* part_ml;                    // maximum (of the scores times scale_log2) and sum
-    struct PagedRecord* records;
+    PagedRecord* records;
     int32_t inject_skip_loads;
 };
 
-// Of a CTA that ends a query tile which an earlier one began: where its parts and its rows are.
-struct PagedRecord {
-    int32_t first;                      // CTA that began it; -1: nothing to join
-    int32_t token0, tokens, head;
-};
-
 // Sequence s of the step.
-template <int kShift>
+template <int kShift, int kItem>
 struct PagedReader {
     const PagedArgs& A;
-    __device__ __forceinline__ void operator()(int s, SeqWork<kShift>& w, int& begin) const
+    __device__ __forceinline__ void operator()(int s, SeqWork<kShift, kItem>& w, int& begin) const
     {
         begin = __ldcg(A.cu_seqlens + s);
         int lq = __ldcg(A.cu_seqlens + s + 1) - begin, len = max(0, __ldcg(A.seq_lens + s));
@@ -45,16 +46,16 @@ struct PagedReader {
 };
 
 // Called by all kThreads threads of a CTA; `scratch` holds a number for each of its warps, in shared memory.
-template <int kThreads, int kShift>
-__device__ __noinline__ void paged_find_run(const PagedArgs& A, int64_t* scratch, PagedRun<kShift>* run)
+template <int kThreads, int kShift, int kItem>
+__device__ __noinline__ void paged_find_run(const PagedArgs& A, int64_t* scratch, PagedRun<kShift, kItem>* run)
 {
-    const PagedReader<kShift> read{A};
+    const PagedReader<kShift, kItem> read{A};
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     constexpr int kWarps = kThreads / 32;
-    const int per = (A.n_seqs + kThreads - 1) / kThreads, s0 = min(tid * per, A.n_seqs), s1 = min(s0 + per, A.n_seqs);
+    const int per = A.n_seqs <= kThreads ? 1 : (A.n_seqs + kThreads - 1) / kThreads, s0 = min(tid * per, A.n_seqs), s1 = min(s0 + per, A.n_seqs);
     int64_t mine = 0, per_head = 0;
     int begin = 0;
-    SeqWork<kShift> w;
+    SeqWork<kShift, kItem> w;
     for (int s = s0; s < s1; ++s) {
         read(s, w, begin);
         per_head = w.units_per_head();
@@ -76,26 +77,29 @@ __device__ __noinline__ void paged_find_run(const PagedArgs& A, int64_t* scratch
         total += scratch[i];
     }
     const int64_t ctas = min(static_cast<int64_t>(gridDim.x), total), c = blockIdx.x;
-    if (c < ctas && mine > 0) {
-        const PagedShares shares(total, ctas);
-        int64_t off = shares.first(c) - before;
-        if (off >= 0 && off < mine) {
-            int s = s0;
-            for (; per > 1 && s < s1; ++s) {          // with one sequence a thread it is at hand
-                read(s, w, begin);
-                per_head = w.units_per_head();
-                if (off < per_head * A.Hkv) break;
-                off -= per_head * A.Hkv;
-            }
-            paged_begin_run(w, s, begin, per_head, off, shares, c, run);
+    if (c >= ctas) return;                    // the whole block
+    const PagedShares shares(total, ctas);
+    int64_t off = shares.first(c) - before;
+    if (off >= 0 && off < mine) {
+        int s = s0;
+        for (; per > 1 && s < s1; ++s) {      // with one sequence a thread it is at hand
+            read(s, w, begin);
+            per_head = w.units_per_head();
+            if (off < per_head * A.Hkv) break;
+            off -= per_head * A.Hkv;
         }
+        paged_begin_run(w, s, begin, per_head, off, shares, c, run);
     }
+    __syncthreads();
+    const int tiles = run->w.tiles;
+    for (int i = tid; i < tiles; i += kThreads)
+        if (paged_begin_tile(i, shares, c, run)) break;
     __syncthreads();
 }
 
 // Keys that token i of the segment's tile sees
-template <int kShift>
-__device__ __forceinline__ int paged_limit(const PagedSegment<kShift>& g, int i)
+template <int kShift, int kItem>
+__device__ __forceinline__ int paged_limit(const PagedSegment<kShift, kItem>& g, int i)
 {
     return g.w.causal ? max(0, min(g.w.len, g.base + i + 1)) : g.w.len;
 }

@@ -91,6 +91,9 @@ def test_strides(lens, Hq, Hkv):
     table[:, :-9] = p.d_table
     binding.efq_paged_attention_fwd(wide[:, 1:Hq + 1, 64:], p.d_k_cache, p.d_v_cache, table, p.d_cu, p.d_seq_lens, p.max_q, o=out[:, ::2])
     assert torch.equal(out[:, ::2], want[0]) and (out[:, 1::2] == 7.0).all()
+    odd = torch.full((p.total, Hq, D + 8), 7.0, dtype=p.dtype, device="cuda")      # rows on 16 bytes and no more
+    binding.efq_paged_attention_fwd(p.d_q, p.d_k_cache, p.d_v_cache, *p.tables, p.max_q, o=odd[..., 8:])
+    assert torch.equal(odd[..., 8:], want[0]) and (odd[..., :8] == 7.0).all()
 
 
 @pytest.mark.parametrize("lens,Hq", [([(8, 3), (1, 0), (2, 500)], 2), ([(300, 100), (64, 0), (5, 5)], 2), ([(40, 1)], 32)])
