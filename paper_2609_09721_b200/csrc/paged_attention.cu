@@ -141,16 +141,46 @@ EncodeTiled encode_tiled()
     return reinterpret_cast<EncodeTiled>(p);
 }
 
-// Box of 64 channels x `box` rows of dimension 1; strides in elements, as the dimensions 1, 2, 3 have them.
-bool encode_rows(CUtensorMap* map, int dtype, const void* base, int rank, const uint64_t* dims, const int64_t* strides, const uint32_t* box)
+bool encode(CUtensorMap* map, int dtype, const void* base, int rank, const uint64_t* dims, const uint64_t* strides, const uint32_t* box)
 {
-    cuuint64_t bytes[3];
-    cuuint32_t ones[4] = {1, 1, 1, 1};
-    for (int i = 0; i + 1 < rank; ++i) bytes[i] = dims[i + 1] > 1 ? static_cast<cuuint64_t>(strides[i]) * 2 : 256;      // a dimension of one is never stepped along
-    const EncodeTiled encode = encode_tiled();
-    return encode != nullptr && encode(map, dtype == EFQ_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, static_cast<cuuint32_t>(rank),
-                                  const_cast<void*>(base), dims, bytes, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    const cuuint32_t ones[5] = {1, 1, 1, 1, 1};
+    const EncodeTiled f = encode_tiled();
+    return f != nullptr && f(map, dtype == EFQ_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, static_cast<cuuint32_t>(rank),
+                             const_cast<void*>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Queries: 64 channels x the heads of a KV group x `tokens`.  Strides in elements.
+bool encode_queries(CUtensorMap* map, int dtype, const efq_rows_t& q, int64_t total, int G, int tokens)
+{
+    const uint64_t dims[3] = {kPagedD, static_cast<uint64_t>(q.heads), static_cast<uint64_t>(total)};
+    const uint64_t strides[2] = {q.heads > 1 ? static_cast<uint64_t>(q.src_head) * 2 : 256, total > 1 ? static_cast<uint64_t>(q.src_token) * 2 : 256};
+    const uint32_t box[3] = {64, static_cast<uint32_t>(G), static_cast<uint32_t>(tokens)};
+    return encode(map, dtype, q.src, 3, dims, strides, box);
+}
+
+// One of the cache's two tensors: 64 channels, 8 tokens, halves of the channels, groups of 8 tokens, place; `rows` tokens a copy.  The place is
+// page * page_step + head * head_step in units of the greatest common divisor of their strides.
+efq_status_t encode_cache(CUtensorMap* map, int dtype, const void* base, int64_t page, int64_t head, int64_t token, const efq_paged_t& c, int rows,
+                          int32_t* page_step, int32_t* head_step)
+{
+    if (c.n_heads == 1) head = 0;
+    if (c.n_pages == 1) page = 0;
+    int64_t unit = page, rest = head;
+    while (rest != 0) {
+        const int64_t x = unit % rest;
+        unit = rest;
+        rest = x;
+    }
+    if (unit == 0) unit = 8;
+    const int64_t places = (c.n_pages - 1) * (page / unit) + (c.n_heads - 1) * (head / unit) + 1;
+    if (places >= (1ll << 31)) return EFQ_ERR_UNSUPPORTED;
+    *page_step = static_cast<int32_t>(page / unit);
+    *head_step = static_cast<int32_t>(head / unit);
+    const uint64_t dims[5] = {64, 8, 2, static_cast<uint64_t>(c.page_size / 8), static_cast<uint64_t>(places)};
+    const uint64_t strides[4] = {static_cast<uint64_t>(token) * 2, 128, static_cast<uint64_t>(token) * 16, static_cast<uint64_t>(unit) * 2};
+    const uint32_t box[5] = {64, 8, 2, static_cast<uint32_t>((c.page_size < rows ? c.page_size : rows) / 8), 1};
+    return encode(map, dtype, base, 5, dims, strides, box) ? EFQ_OK : EFQ_ERR_CUDA;
 }
 
 struct PagedPlan {
@@ -160,7 +190,7 @@ struct PagedPlan {
 PagedPlan plan_paged(int64_t group_rows)
 {
     PagedPlan p;
-    p.rows = group_rows <= 16 ? 16 : group_rows <= 32 ? 32 : 2 * kChunkRows;
+    p.rows = group_rows <= kFewRows ? kFewRows : 2 * kChunkRows;
     p.ml = static_cast<size_t>(2 * kMaxCtas) * p.rows * kPagedD * 4;
     p.records = p.ml + static_cast<size_t>(2 * kMaxCtas) * p.rows * sizeof(float2);
     p.total = p.records + kMaxCtas * sizeof(PagedRecord);       // records on 16 bytes: 2 * kMaxCtas * rows is a multiple of 8
@@ -177,14 +207,14 @@ cudaError_t allow_smem(Kernel kernel, int bytes, std::atomic<uint64_t>& done, in
     return e;
 }
 
-template <typename T, int kM>
+template <typename T>
 cudaError_t launch_few_rows(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const PagedArgs& A, int ctas, int max_rows, int dev, cudaStream_t st)
 {
     static std::atomic<uint64_t> done{0};
-    constexpr int smem = static_cast<int>(sizeof(FewSmem<kM>)) + 1024;
-    cudaError_t e = allow_smem(paged_few_kernel<T, kM>, smem, done, dev);
-    if (e == cudaSuccess) e = launch_overlapped(paged_few_kernel<T, kM>, dim3(static_cast<unsigned>(ctas)), kFewThreads, smem, st, mq, mk, mv, A);
-    if (e == cudaSuccess) e = launch_overlapped(paged_join_kernel<T, 16 * kM>, dim3(static_cast<unsigned>(ctas), static_cast<unsigned>(max_rows)), 128, 0, st, A);
+    constexpr int smem = static_cast<int>(sizeof(FewSmem)) + 1024;
+    cudaError_t e = allow_smem(paged_few_kernel<T>, smem, done, dev);
+    if (e == cudaSuccess) e = launch_overlapped(paged_few_kernel<T>, dim3(static_cast<unsigned>(ctas)), kFewThreads, smem, st, mq, mk, mv, A);
+    if (e == cudaSuccess) e = launch_overlapped(paged_join_kernel<T, kFewRows>, dim3(static_cast<unsigned>(ctas), static_cast<unsigned>(max_rows)), 128, 0, st, A);
     return e;
 }
 
@@ -249,28 +279,22 @@ efq_status_t paged_attention(const efq_rows_t* q, float* lse, int64_t total, int
     A.part_ml = reinterpret_cast<float2*>(ws + plan.ml);
     A.records = reinterpret_cast<PagedRecord*>(ws + plan.records);
     A.inject_skip_loads = inject_skip_loads ? 1 : 0;
-    const bool many = plan.rows > 32;
+    const bool many = plan.rows > kFewRows;
     A.step = many ? kChunkRows / G * 2 : plan.rows / G;
 
     CUtensorMap mq, mk, mv;
-    const uint64_t q_dims[3] = {kPagedD, static_cast<uint64_t>(q->heads), static_cast<uint64_t>(total)};
-    const int64_t q_strides[2] = {q->src_head, q->src_token};
-    const uint32_t q_box[3] = {64, static_cast<uint32_t>(G), static_cast<uint32_t>(many ? A.step / 2 : A.step)};
-    const uint64_t dims[4] = {kPagedD, static_cast<uint64_t>(cache->page_size), static_cast<uint64_t>(cache->n_heads), static_cast<uint64_t>(cache->n_pages)};
-    const int64_t k_strides[3] = {cache->k_token, cache->k_head, cache->k_page}, v_strides[3] = {cache->v_token, cache->v_head, cache->v_page};
     const int keys = many ? kChunkKeys : kFewKeys;
-    const uint32_t box[4] = {64, static_cast<uint32_t>(cache->page_size < keys ? cache->page_size : keys), 1, 1};
-    if (!encode_rows(&mq, dtype, q->src, 3, q_dims, q_strides, q_box) || !encode_rows(&mk, dtype, cache->k, 4, dims, k_strides, box) ||
-        !encode_rows(&mv, dtype, cache->v, 4, dims, v_strides, box))
-        return EFQ_ERR_CUDA;
+    if (!encode_queries(&mq, dtype, *q, total, G, many ? A.step / 2 : A.step)) return EFQ_ERR_CUDA;
+    efq_status_t map_status = encode_cache(&mk, dtype, cache->k, cache->k_page, cache->k_head, cache->k_token, *cache, keys, &A.k_page_step, &A.k_head_step);
+    if (map_status == EFQ_OK)
+        map_status = encode_cache(&mv, dtype, cache->v, cache->v_page, cache->v_head, cache->v_token, *cache, keys, &A.v_page_step, &A.v_head_step);
+    if (map_status != EFQ_OK) return map_status;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const int max_rows = group_rows < A.step * G ? static_cast<int>(group_rows) : A.step * G;       // the join's blocks; with more rows they go round
     using Bf = __nv_bfloat16;
     const bool bf = dtype == EFQ_BF16;
     const cudaError_t e = many ? (bf ? launch_chunk<Bf>(mq, mk, mv, A, ctas, dev, s) : launch_chunk<__half>(mq, mk, mv, A, ctas, dev, s))
-                          : plan.rows == 16
-                              ? (bf ? launch_few_rows<Bf, 1>(mq, mk, mv, A, ctas, max_rows, dev, s) : launch_few_rows<__half, 1>(mq, mk, mv, A, ctas, max_rows, dev, s))
-                              : (bf ? launch_few_rows<Bf, 2>(mq, mk, mv, A, ctas, max_rows, dev, s) : launch_few_rows<__half, 2>(mq, mk, mv, A, ctas, max_rows, dev, s));
+                               : (bf ? launch_few_rows<Bf>(mq, mk, mv, A, ctas, max_rows, dev, s) : launch_few_rows<__half>(mq, mk, mv, A, ctas, max_rows, dev, s));
     return e == cudaSuccess ? EFQ_OK : EFQ_ERR_CUDA;
 }
 

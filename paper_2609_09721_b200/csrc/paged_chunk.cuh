@@ -26,7 +26,7 @@ constexpr float kSlack = 8.0f;                                 // log2: probabil
 
 struct __align__(1024) ChunkSmem {
     uint8_t q[2][2][kChunkPart];                               // half, channels 0-63 and 64-127; 128-byte swizzle
-    uint8_t kv[kChunkSlots][2][kChunkPart];
+    uint8_t kv[kChunkSlots][2 * kChunkPart];                   // [8 tokens][channels 0-63, 64-127][token]
     uint64_t full[kChunkSlots], empty[kChunkSlots], q_full, q_empty, s_full[2], p_ready[2], p_rest[2], o_full[2], v_tail, v_clean, turn[2], drained[2];
     int64_t scratch[kChunkThreads / 32];
     PagedRun<kChunkShift, kChunkItem> run;
@@ -174,7 +174,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
                 };
                 // One operand of a tile: lane i takes its i-th page.  Where an entry is no page, the rows of K are NaN, which makes rows of
                 // NaN of the queries that see them, and the rows of V are 0.
-                auto load = [&](const CUtensorMap& map, int j, int at, uint32_t fill) {
+                auto load = [&](const CUtensorMap& map, int page_step, int head_step, int j, int at, uint32_t fill) {
                     const int entry = at < A.n_pages ? at : -1;
                     const uint32_t s = slot % kChunkSlots;
                     if (slot >= kChunkSlots) ok = paged_wait_warp(&sm->empty[s], (slot / kChunkSlots - 1) & 1u, sm);
@@ -182,26 +182,20 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
                     const int key = j * kChunkKeys + row;
                     const bool mine = row < kChunkKeys && key < g.w.len, page = mine && entry >= 0 && !A.inject_skip_loads;
                     if (mine && entry < 0) {
-    #pragma unroll 1
-                    for (int i = 0; i < box * 8; ++i) {
-                            reinterpret_cast<uint4*>(sm->kv[s][0] + row * 128)[i] = make_uint4(fill, fill, fill, fill);
-                            reinterpret_cast<uint4*>(sm->kv[s][1] + row * 128)[i] = make_uint4(fill, fill, fill, fill);
-                        }
+#pragma unroll 1
+                        for (int i = 0; i < box * 16; ++i) reinterpret_cast<uint4*>(sm->kv[s] + row * 256)[i] = make_uint4(fill, fill, fill, fill);
                         ptx::fence_proxy_async_smem();
                     }
                     const uint32_t pages = __popc(__ballot_sync(0xffffffffu, page));
                     if (lane == 0) ptx::mbar_arrive_expect_tx(&sm->full[s], (A.inject_skip_loads ? 1u : pages) * static_cast<uint32_t>(box) * 256u);
                     __syncwarp();
-                    if (page) {
-                        tma_load_4d(sm->kv[s][0] + row * 128, &map, 0, key & (P - 1), g.head, entry, &sm->full[s]);
-                        tma_load_4d(sm->kv[s][1] + row * 128, &map, 64, key & (P - 1), g.head, entry, &sm->full[s]);
-                    }
+                    if (page) tma_load_page(sm->kv[s] + row * 256, &map, (key & (P - 1)) >> 3, entry * page_step + g.head * head_step, &sm->full[s]);
                     ++slot;
                 };
                 int entry = entry_of(g.j0), next = entry_of(g.j0 + 1);
                 for (int j = g.j0; ok && j < end; ++j) {
                     const int ahead = entry_of(j + 2);
-                    load(mk, j, entry, 0x7fff7fffu);
+                    load(mk, A.k_page_step, A.k_head_step, j, entry, 0x7fff7fffu);
                     if (ok && j == g.j0) {
                         if (q_loads > 0) ok = paged_wait_warp(&sm->q_empty, (q_loads - 1) & 1u, sm);
                         if (!ok) break;
@@ -214,7 +208,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
                         __syncwarp();
                         ++q_loads;
                     }
-                    if (ok) load(mv, j, entry, 0u);
+                    if (ok) load(mv, A.v_page_step, A.v_head_step, j, entry, 0u);
                     entry = next;
                     next = ahead;
                 }
@@ -236,8 +230,8 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
             const int w = uniform(warp == 11 ? 1 : 0);
             const uint32_t tm = uniform(tmem), s_tmem = tm + kChunkColS + 128 * w, o_tmem = tm + kChunkColO + 128 * w;
             const uint64_t dq = ptx::smem_desc(ptx::smem_u32(sm->q[0][0]) + w * 2 * kChunkPart, 16, 1024, ptx::kLayoutSw128);
-            const uint64_t dk = ptx::smem_desc(ptx::smem_u32(sm->kv[0][0]), 16, 1024, ptx::kLayoutSw128);
-            const uint64_t dv = ptx::smem_desc(ptx::smem_u32(sm->kv[0][0]), kChunkPart, 1024, ptx::kLayoutSw128);
+            const uint64_t dk = ptx::smem_desc(ptx::smem_u32(sm->kv[0]), 16, 2048, ptx::kLayoutSw128);
+            const uint64_t dv = ptx::smem_desc(ptx::smem_u32(sm->kv[0]), 1024, 2048, ptx::kLayoutSw128);
             constexpr uint32_t kSlotStep = 2 * kChunkPart >> 4;
             uint64_t *const s_full = &sm->s_full[w], *const p_ready = &sm->p_ready[w], *const p_rest = &sm->p_rest[w], *const o_full = &sm->o_full[w];
             uint64_t *const turn_mine = &sm->turn[w], *const turn_other = &sm->turn[w ^ 1];
@@ -265,8 +259,8 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
                 const uint64_t k = dk + slot * kSlotStep;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const uint32_t off = ((i >> 2) * kChunkPart + (i & 3) * 32) >> 4;
-                    ptx::mma_bf16(s_tmem, dq + off, k + off, chunk_idesc<T>(false), i > 0 ? 1u : 0u);
+                    const uint32_t off = ((i >> 2) * kChunkPart + (i & 3) * 32) >> 4, k_off = ((i >> 2) * 1024 + (i & 3) * 32) >> 4;
+                    ptx::mma_bf16(s_tmem, dq + off, k + k_off, chunk_idesc<T>(false), i > 0 ? 1u : 0u);
                     if (i == 4) ptx::mbar_arrive(turn_other);
                 }
                 ptx::mma_commit(s_full);
@@ -313,7 +307,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
                         if (ptx::elect_one()) {
 #pragma unroll
                             for (int i = 0; i < 6; ++i)
-                                ptx::mma_bf16_ts(o_tmem, s_tmem + 8 * i, v + (i * 2048u >> 4), chunk_idesc<T>(true), i > 0 || j > j0 ? 1u : 0u);
+                                ptx::mma_bf16_ts(o_tmem, s_tmem + 8 * i, v + (i * 4096u >> 4), chunk_idesc<T>(true), i > 0 || j > j0 ? 1u : 0u);
                         }
                         __syncwarp();
                         ok = paged_wait_warp(p_rest, p_round, sm);
@@ -322,7 +316,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
                         ptx::tc_fence_after_sync();
                         if (ptx::elect_one()) {
 #pragma unroll
-                            for (int i = 6; i < 8; ++i) ptx::mma_bf16_ts(o_tmem, s_tmem + 8 * i, v + (i * 2048u >> 4), chunk_idesc<T>(true), 1u);
+                            for (int i = 6; i < 8; ++i) ptx::mma_bf16_ts(o_tmem, s_tmem + 8 * i, v + (i * 4096u >> 4), chunk_idesc<T>(true), 1u);
                             if (j + 1 < mine) {
                                 scores();
                             } else {
@@ -367,11 +361,11 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
                 ok = paged_wait_warp(&sm->v_tail, round, sm);
                 if (!ok) break;
                 round ^= 1u;
-                uint8_t* const v = sm->kv[(slot - 1) % kChunkSlots][0];
+                uint8_t* const v = sm->kv[(slot - 1) % kChunkSlots];
 #pragma unroll 1
-                for (int i = inside * 8 + lane; i < kChunkKeys * 8; i += 32) {
-                    reinterpret_cast<uint4*>(v)[i] = make_uint4(0u, 0u, 0u, 0u);
-                    reinterpret_cast<uint4*>(v + kChunkPart)[i] = make_uint4(0u, 0u, 0u, 0u);
+                for (int i = inside * 16 + lane; i < kChunkKeys * 16; i += 32) {       // 16 bytes: row i / 16, channels from 8 (i % 16) on
+                    const int r = i >> 4;
+                    *reinterpret_cast<uint4*>(v + (r >> 3) * 2048 + ((i >> 3) & 1) * 1024 + (r & 7) * 128 + (i & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
                 }
                 ptx::fence_proxy_async_smem();
                 __syncwarp();

@@ -18,6 +18,7 @@ struct PagedArgs {
     const int32_t *page_table, *cu_seqlens, *seq_lens;
     int64_t table_stride;
     int32_t n_seqs, n_pages, max_pages, page_shift;
+    int32_t k_page_step, k_head_step, v_page_step, v_head_step;      // of the copies' last coordinate
     int32_t Hkv, G, causal, total;
     int32_t step;                       // new tokens of a query tile
     float scale_log2;                   // softmax scale / ln 2
