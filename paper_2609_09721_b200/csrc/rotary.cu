@@ -15,8 +15,11 @@
 namespace efq {
 namespace {
 
-constexpr int kWarps = 8;               // of a block
-constexpr int kRowsAhead = 4;           // rows a lane has in flight
+constexpr int kWarps = 4;               // of a block
+// Rows a lane has in flight.  Two leave 32 warps to an SM, four 20: 24 + 24 heads of 32760 tokens 132.2 us and 129.9, of 4097 tokens, which
+// the 32 warps take in one go, 20.6 and 22.6, a chunk of 8192 tokens into the cache 37.7 and 37.1.  Asking for the first rows before the angles
+// are made costs time (32760 tokens 135 and 151 us), as do angles shared by a block instead of a warp (142).
+constexpr int kRowsAhead = 2;
 
 struct RotaryRows {
     const char* src;
@@ -55,7 +58,7 @@ __device__ __forceinline__ int find_sequence(const int32_t* cu, int n_seqs, int6
 }
 
 template <typename T, bool kInterleaved, bool kPaged>
-__global__ void __launch_bounds__(kWarps * 32) rotary_kernel(const __grid_constant__ RotaryArgs A)
+__global__ void __launch_bounds__(kWarps * 32, 8) rotary_kernel(const __grid_constant__ RotaryArgs A)
 {
     ptx::grid_wait();
     const int lane = threadIdx.x & 31;
