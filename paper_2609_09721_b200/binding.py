@@ -1,6 +1,7 @@
 """Python binding of libefq_b200.so: same names as the C ABI in include/efq.h.
 
-Argument marshalling only: ctypes, and for the calls of a serving loop the CPython extension efq_fastcall.  Tensors are
+Argument marshalling only: ctypes, and for the calls of a serving loop the CPython extensions efq_fastcall and, where many tensors are
+described, efq_tensorcall.  Tensors are
 torch CUDA tensors (torch is used for device memory and streams); nothing here computes.  There is no CPU fallback: if the
 library has not been built, or a call returns a non-zero status, a RuntimeError is raised.
 """
@@ -68,6 +69,7 @@ class EfqError(RuntimeError):
 
 _lib = None
 _fast = None
+_tensors = None
 _raw_stream, _raw_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice    # a tenth of torch.cuda.current_stream()
 
 
@@ -159,9 +161,23 @@ def _fastcall():
         efq_fastcall.set_functions(address(L.efq_attention_fwd), address(L.exp_then_quantize_attention_fwd),
                                    address(L.efq_probgen), address(L.exp_then_quantize_probgen),
                                    address(L.efq_attention_fwd_varlen), address(L.efq_attention_varlen_workspace_bytes))
-        efq_fastcall.set_paged_functions(address(L.efq_rotary), address(L.efq_paged_append), address(L.efq_paged_attention_fwd))
         _fast = efq_fastcall
     return _fast
+
+
+def _tensorcall():
+    """The extension that calls the operators around a paged cache with tensors; raises if it has not been built."""
+    global _tensors
+    if _tensors is None:
+        L = lib()
+        try:
+            from . import efq_tensorcall
+        except ImportError as e:
+            raise RuntimeError("efq_tensorcall.so is missing: build it with `python -m paper_2609_09721_b200.build`") from e
+        address = lambda f: C.cast(f, C.c_void_p).value
+        efq_tensorcall.set_functions(address(L.efq_rotary), address(L.efq_paged_append), address(L.efq_paged_attention_fwd))
+        _tensors = efq_tensorcall
+    return _tensors
 
 
 def status_string(status: int) -> str:
@@ -451,9 +467,6 @@ def efq_calibrate(q, k, v, o_ref, taus, hs, causal: bool = False, softmax_scale:
     return table, (float(bt.value), float(bh.value))
 
 
-_ELEMENTS = {torch.bfloat16: 0, torch.float16: 1}
-
-
 class Rotary:
     """Rotary positions with one to four axes, as efq_rotary and efq_paged_append take them: made once and kept.
 
@@ -466,7 +479,11 @@ class Rotary:
         assert min(sections) >= 0 and inv_freq.numel() == sum(sections)
         self.inv_freq, self.sections = inv_freq, sections
         self.c = EfqRotary(inv_freq.data_ptr(), len(sections), (C.c_int32 * 4)(*sections), int(bool(interleaved)))
-        self.address = C.addressof(self.c)
+        self._address, self._device = C.addressof(self.c), inv_freq.get_device()
+
+    def address_on(self, device: int) -> int:
+        assert self._device == device, "the rotation's frequencies have to be on the current CUDA device"
+        return self._address
 
     @classmethod
     def of(cls, sections, theta: float = 10000.0, interleaved: bool = False, ladder_per_axis: bool = False, device=None):
@@ -476,89 +493,31 @@ class Rotary:
         return cls(torch.tensor([float(theta) ** -x for x in steps], dtype=torch.float64, device=device or "cuda"), sections, interleaved)
 
 
-def _here(*tensors):
-    """The tensors are on the current device, whose streams the call uses."""
-    device = _raw_device()
-    for t in tensors:
-        assert t.get_device() == device, "tensors have to be on the current CUDA device"
-
-
-def _turned_out(x, out):
-    if out is None:
-        return torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    assert out.shape == x.shape and out.dtype is x.dtype and out.stride(-1) == 1
-    return out
+def _out(x, out):
+    return torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None and x is not None else out
 
 
 def efq_rotary(q, k, positions, rotary: Rotary, inverse: bool = False, q_out=None, k_out=None, stream=None):
     """Rotary positions turned into q [B, Hq, S, 128] and k [B, Hkv, S, 128] (bf16 or fp16, any strides; either may be None) in one
     launch.  positions: int32 [axes, S], or [axes, B, S].  q_out and k_out: the outputs (q and k themselves: in place); new tensors are
     contiguous, as the forwards take them.  inverse: turned back, which is the gradient.  Returns (q_out, k_out)."""
-    x = q if q is not None else k
-    B, _, S, d = x.shape
-    assert d == 128 and positions.dtype is torch.int32 and positions.stride(-1) == 1 and positions.shape[0] == len(rotary.sections)
-    assert positions.shape[1:] in ((S,), (B, S))
-    _here(x, positions, rotary.inv_freq)
-    args = []
-    outs = []
-    for t, out in ((q, q_out), (k, k_out)):
-        if t is None:
-            args += (None, None, None, None, None)
-            outs.append(None)
-            continue
-        out = _turned_out(t, out)
-        assert t.shape[0] == B and t.shape[2] == S and t.shape[3] == d and t.dtype is x.dtype and (t.stride(3) == 1 or t.numel() == 0)
-        _here(t, out)
-        args += (t.data_ptr(), out.data_ptr(), t.shape, t.stride(), out.stride())
-        outs.append(out)
-    st = (_fast or _fastcall()).rotary(*args, positions.data_ptr(), positions.stride(0), positions.stride(1) if positions.dim() == 3 else 0, B, S,
-                                       _ELEMENTS[x.dtype], rotary.address, 1 if inverse else 0, _stream(stream))
+    q_out, k_out = _out(q, q_out), _out(k, k_out)
+    st = (_tensors or _tensorcall()).rotary(q, k, positions, rotary.address_on(_raw_device()), 1 if inverse else 0, q_out, k_out, _raw_device(), _stream(stream))
     if st:
         _check(st, "efq_rotary")
-    return tuple(outs)
-
-
-def _cache_args(k_cache, v_cache, page_table, cu_seqlens, seq_lens, dtype):
-    """The cache [pages, Hkv, page_size, 128] and the step's int32 tables: page_table [n_seqs, max_pages], cu_seqlens [n_seqs + 1], seq_lens [n_seqs]."""
-    shape, table = k_cache.shape, page_table.shape
-    assert k_cache.dtype is dtype and v_cache.dtype is dtype and v_cache.shape == shape and len(shape) == 4 and shape[3] == 128
-    assert k_cache.stride(3) == 1 and v_cache.stride(3) == 1
-    i32 = torch.int32
-    assert page_table.dtype is i32 and cu_seqlens.dtype is i32 and seq_lens.dtype is i32
-    assert len(table) == 2 and page_table.stride(1) == 1 and cu_seqlens.shape == (table[0] + 1,) and seq_lens.shape == (table[0],)
-    assert cu_seqlens.is_contiguous() and seq_lens.is_contiguous()
-    _here(k_cache, v_cache, page_table, cu_seqlens, seq_lens)
-    return (k_cache.data_ptr(), v_cache.data_ptr(), shape, k_cache.stride(), v_cache.stride(), page_table.data_ptr(), table, page_table.stride(),
-            cu_seqlens.data_ptr(), seq_lens.data_ptr())
+    return (None if q is None else q_out), (None if k is None else k_out)
 
 
 def efq_paged_append(k, v, k_cache, v_cache, page_table, cu_seqlens, seq_lens, rotary: Optional[Rotary] = None, positions=None, q=None,
                      q_out=None, stream=None):
     """Writes the new keys (rotated) and values of a step, [total, Hkv, 128], into the paged cache [pages, Hkv, page_size, 128] and
-    rotates q [total, Hq, 128] beside them.  cu_seqlens, seq_lens, page_table: int32 CUDA tensors; seq_lens counts the new tokens too.
-    positions: int32 [axes, total], None: a token's index in its sequence.  Returns q_out, or None without q."""
-    total, Hkv, d = k.shape
-    dtype = k.dtype
-    assert v.shape == k.shape and v.dtype is dtype and d == 128 and Hkv == k_cache.shape[1]
-    assert (k.stride(2) == 1 and v.stride(2) == 1) or total == 0
-    _here(k, v)
-    cache = _cache_args(k_cache, v_cache, page_table, cu_seqlens, seq_lens, dtype)
-    if rotary is not None:
-        _here(rotary.inv_freq)
-    if positions is not None:
-        assert rotary is not None and positions.dtype is torch.int32 and positions.shape == (len(rotary.sections), total)
-        assert positions.stride(1) == 1 or total <= 1
-        _here(positions)
-    q_args = (None, None, None, None, None)
-    if q is not None:
-        assert q.dim() == 3 and q.shape[0] == total and q.shape[2] == d and q.dtype is dtype and (q.stride(2) == 1 or total == 0)
-        q_out = _turned_out(q, q_out)
-        _here(q, q_out)
-        q_args = (q.data_ptr(), q_out.data_ptr(), q.shape, q.stride(), q_out.stride())
-    ks, vs = k.stride(), v.stride()
-    st = (_fast or _fastcall()).paged_append(k.data_ptr(), None, k.shape, ks, ks, v.data_ptr(), None, v.shape, vs, vs, *q_args, total,
-                                             None if positions is None else positions.data_ptr(), 0 if positions is None else positions.stride(0),
-                                             *cache, _ELEMENTS[dtype], None if rotary is None else rotary.address, _stream(stream))
+    rotates q [total, Hq, 128] beside them.  cu_seqlens [n_seqs + 1], seq_lens [n_seqs], page_table [n_seqs, max_pages]: int32 CUDA tensors;
+    seq_lens counts the new tokens too.  positions: int32 [axes, total], None: a token's index in its sequence.  Returns q_out, or None
+    without q."""
+    q_out = _out(q, q_out)
+    device = _raw_device()
+    st = (_tensors or _tensorcall()).paged_append(k, v, k_cache, v_cache, page_table, cu_seqlens, seq_lens, None if rotary is None else rotary.address_on(device),
+                                                  positions, q, q_out, device, _stream(stream))
     if st:
         _check(st, "efq_paged_append")
     return None if q is None else q_out
@@ -568,33 +527,33 @@ def efq_paged_attention_workspace_bytes(Hq: int, Hkv: int, max_seqlen_q: int, d:
     return int(lib().efq_paged_attention_workspace_bytes(Hq, Hkv, max_seqlen_q, d))
 
 
-def _paged_attention_args(q, k_cache, v_cache, page_table, cu_seqlens, seq_lens, max_seqlen_q, o, lse, workspace):
-    total, Hq, d = q.shape
-    dtype = q.dtype
-    assert d == 128 and (q.stride(2) == 1 or total == 0)
-    o = _turned_out(q, o)
-    _here(q, o)
-    cache = _cache_args(k_cache, v_cache, page_table, cu_seqlens, seq_lens, dtype)
-    if lse is not None:
-        assert lse.dtype is torch.float32 and lse.shape == (total, Hq) and lse.is_contiguous()
-        _here(lse)
-    if workspace is None:
-        workspace = torch.empty(max(efq_paged_attention_workspace_bytes(Hq, k_cache.shape[1], max_seqlen_q, d), 256), dtype=torch.uint8, device=q.device)
-    _here(workspace)
-    return total, o, cache, workspace
+def _paged_workspace(q, k_cache, max_seqlen_q):
+    n = efq_paged_attention_workspace_bytes(q.shape[1], k_cache.shape[1], max_seqlen_q, q.shape[2]) if q.dim() == 3 and k_cache.dim() == 4 else 0
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=q.device)
 
 
 def efq_paged_attention_fwd(q, k_cache, v_cache, page_table, cu_seqlens, seq_lens, max_seqlen_q: int, causal: bool = True,
                             softmax_scale: float = 0.0, o=None, lse=None, workspace=None, stream=None):
     """Softmax attention of a step's new tokens q [total, Hq, 128] over a paged cache [pages, Hkv, page_size, 128] (tables as for
     efq_paged_append); max_seqlen_q: the most new tokens of any sequence.  lse: optional fp32 [total, Hq] output.  Returns o, of q's type."""
-    total, o, cache, workspace = _paged_attention_args(q, k_cache, v_cache, page_table, cu_seqlens, seq_lens, max_seqlen_q, o, lse, workspace)
-    st = (_fast or _fastcall()).paged_attention(q.data_ptr(), o.data_ptr(), q.shape, q.stride(), o.stride(), None if lse is None else lse.data_ptr(), total,
-                                                max_seqlen_q, *cache, _ELEMENTS[q.dtype], 1 if causal else 0, softmax_scale, workspace.data_ptr(),
-                                                workspace.numel(), _stream(stream))
+    o = _out(q, o)
+    if workspace is None:
+        workspace = _paged_workspace(q, k_cache, max_seqlen_q)
+    st = (_tensors or _tensorcall()).paged_attention(q, k_cache, v_cache, page_table, cu_seqlens, seq_lens, max_seqlen_q, 1 if causal else 0, softmax_scale, o, lse,
+                                                     workspace, _raw_device(), _stream(stream))
     if st:
         _check(st, "efq_paged_attention_fwd")
     return o
+
+
+def efq_paged_attention_fwd_inject_timeout(q, k_cache, v_cache, page_table, cu_seqlens, seq_lens, max_seqlen_q: int, o, workspace, stream=None) -> None:
+    """Test hook: efq_paged_attention_fwd without loads of K and V, so that its bounded device-side waits expire; the rows of `o` become NaN."""
+    rows = EfqRows(q.data_ptr(), o.data_ptr(), q.shape[1], 0, q.stride(1), q.stride(0), 0, o.stride(1), o.stride(0))
+    cache = EfqPaged(k_cache.data_ptr(), v_cache.data_ptr(), *k_cache.stride()[:3], *v_cache.stride()[:3], *k_cache.shape[:3], page_table.data_ptr(),
+                     page_table.stride(0), page_table.shape[1], cu_seqlens.data_ptr(), seq_lens.data_ptr(), page_table.shape[0])
+    st = lib().efq_paged_attention_fwd_inject_timeout(C.byref(rows), None, q.shape[0], int(max_seqlen_q), C.byref(cache), q.shape[2],
+                                                      1 if q.dtype == torch.float16 else 0, 1, 0.0, workspace.data_ptr(), workspace.numel(), _stream(stream))
+    _check(st, "efq_paged_attention_fwd_inject_timeout")
 
 
 def efq_poll_status(workspace, stream=None) -> int:

@@ -1,5 +1,5 @@
-"""Builds the C-ABI CUDA library in-tree, paper_2609_09721_b200/libefq_b200.so (sm_100a only), and the CPython extension
-beside it that calls it, efq_fastcall.so."""
+"""Builds the C-ABI CUDA library in-tree, paper_2609_09721_b200/libefq_b200.so (sm_100a only), and the CPython extensions
+beside it that call it: efq_fastcall.so, which takes plain integers, and efq_tensorcall.so, which takes torch tensors."""
 from __future__ import annotations
 
 import glob
@@ -14,6 +14,8 @@ CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libefq_b200.so")
 FASTCALL_SRC = os.path.join(CSRC, "fastcall.c")
 FASTCALL = os.path.join(_HERE, "efq_fastcall.so")
+TENSORCALL_SRC = os.path.join(CSRC, "tensorcall.cpp")
+TENSORCALL = os.path.join(_HERE, "efq_tensorcall.so")
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo",
@@ -26,11 +28,22 @@ def sources():
 
 
 def _stale() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(FASTCALL):
+    built = (LIB, FASTCALL, TENSORCALL)
+    if not all(os.path.exists(f) for f in built):
         return True
-    t = min(os.path.getmtime(LIB), os.path.getmtime(FASTCALL))
-    deps = sources() + [FASTCALL_SRC] + glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(ROOT, "include", "*.h"))
+    t = min(os.path.getmtime(f) for f in built)
+    deps = sources() + [FASTCALL_SRC, TENSORCALL_SRC] + glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(ROOT, "include", "*.h"))
     return any(os.path.getmtime(d) > t for d in deps)
+
+
+def _start_tensorcall(out: str):
+    import torch
+    torch_dir = os.path.dirname(torch.__file__)
+    return subprocess.Popen([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-Wall", "-shared", "-fPIC",
+                             f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", sysconfig.get_paths()["include"],
+                             "-I", os.path.join(ROOT, "include"), "-isystem", os.path.join(torch_dir, "include"), TENSORCALL_SRC, "-o", out,
+                             "-L", os.path.join(torch_dir, "lib"), "-lc10", "-ltorch_cpu", "-ltorch_python"],
+                            stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
@@ -39,6 +52,8 @@ def build(force: bool = False, verbose: bool = False) -> str:
     objs = []
     os.makedirs(os.path.join(_HERE, "build"), exist_ok=True)
     procs = []
+    tensorcall_tmp = TENSORCALL + f".tmp{os.getpid()}"
+    tensorcall = _start_tensorcall(tensorcall_tmp)
     for src in sources():
         obj = os.path.join(_HERE, "build", os.path.basename(src)[:-3] + ".o")
         cmd = [NVCC, *FLAGS, "-c", src, "-o", obj] + (["-Xptxas", "-v"] if verbose else [])
@@ -57,6 +72,12 @@ def build(force: bool = False, verbose: bool = False) -> str:
     subprocess.run([os.environ.get("CC", "gcc"), "-O2", "-Wall", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"],
                     "-I", os.path.join(ROOT, "include"), FASTCALL_SRC, "-o", tmp], check=True)
     os.replace(tmp, FASTCALL)
+    out, _ = tensorcall.communicate()
+    if verbose or tensorcall.returncode != 0:
+        sys.stderr.write(out)
+    if tensorcall.returncode != 0:
+        raise RuntimeError(f"g++ failed on {TENSORCALL_SRC}")
+    os.replace(tensorcall_tmp, TENSORCALL)
     return LIB
 
 

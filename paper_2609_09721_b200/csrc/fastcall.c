@@ -22,12 +22,6 @@ typedef efq_status_t (*varlen_fn)(const void*, const void*, const void*, float*,
                                   int, float, int, const efq_params_t*, void*, size_t, void*);
 typedef size_t (*varlen_bytes_fn)(const int64_t*, const int64_t*, int, int, int, int);
 
-typedef efq_status_t (*rotary_fn)(const efq_rows_t*, const efq_rows_t*, const int32_t*, int64_t, int64_t, int, int64_t, int, int,
-                                  const efq_rotary_t*, int, void*);
-typedef efq_status_t (*paged_append_fn)(const efq_rows_t*, const efq_rows_t*, const efq_rows_t*, int64_t, const int32_t*, int64_t,
-                                        const efq_paged_t*, int, int, const efq_rotary_t*, void*);
-typedef efq_status_t (*paged_attention_fn)(const efq_rows_t*, float*, int64_t, int, const efq_paged_t*, int, int, int, float, void*, size_t, void*);
-
 static struct {
     attention_fn attention;
     etq_attention_fn etq_attention;
@@ -36,11 +30,6 @@ static struct {
     varlen_fn varlen;
     varlen_bytes_fn varlen_bytes;
 } fn;
-static struct {
-    rotary_fn rotary;
-    paged_append_fn append;
-    paged_attention_fn attention;
-} paged_fn;
 
 /* The call without the interpreter lock; its arguments are plain C values by then. */
 #define UNLOCKED(type, call) type st; Py_BEGIN_ALLOW_THREADS st = call; Py_END_ALLOW_THREADS
@@ -182,146 +171,6 @@ static PyObject* varlen(PyObject* self, PyObject* const* a, Py_ssize_t n)
     return result;
 }
 
-static PyObject* set_paged_functions(PyObject* self, PyObject* const* a, Py_ssize_t n)
-{
-    (void)self;
-    if (n != 3) { PyErr_SetString(PyExc_TypeError, "efq_fastcall.set_paged_functions: three addresses expected"); return NULL; }
-    paged_fn.rotary = (rotary_fn)ptr(a[0]);
-    paged_fn.append = (paged_append_fn)ptr(a[1]);
-    paged_fn.attention = (paged_attention_fn)ptr(a[2]);
-    if (PyErr_Occurred()) return NULL;
-    Py_RETURN_NONE;
-}
-
-static int want_paged(Py_ssize_t got, Py_ssize_t n)
-{
-    if (paged_fn.rotary == NULL) { PyErr_SetString(PyExc_RuntimeError, "efq_fastcall: the library's functions have not been set"); return 0; }
-    if (got != n) { PyErr_Format(PyExc_TypeError, "efq_fastcall: %zd arguments expected, got %zd", n, got); return 0; }
-    return 1;
-}
-
-/* A tensor's shape or strides as `n` integers. */
-static int dims(PyObject* o, int64_t* out, Py_ssize_t n)
-{
-    if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != n) { PyErr_Format(PyExc_TypeError, "efq_fastcall: a tuple of %zd integers expected", n); return 0; }
-    for (Py_ssize_t i = 0; i < n; ++i) out[i] = i64(PyTuple_GET_ITEM(o, i));
-    return !PyErr_Occurred();
-}
-
-/* Rows from (src, dst, shape, strides of src, strides of dst); src None: no tensor.  The shapes are [B, H, S, d] or, token-major
- * without a batch, [total, H, d]. */
-#define GROUP 5
-static int rows4(PyObject* const* a, efq_rows_t* r)
-{
-    int64_t shape[4], s[4], t[4];
-    if (a[0] == Py_None) return 0;
-    r->src = ptr(a[0]);
-    r->dst = ptr(a[1]);
-    if (!dims(a[2], shape, 4) || !dims(a[3], s, 4) || !dims(a[4], t, 4)) return -1;
-    r->heads = (int32_t)shape[1];
-    r->src_batch = s[0]; r->src_head = s[1]; r->src_token = s[2];
-    r->dst_batch = t[0]; r->dst_head = t[1]; r->dst_token = t[2];
-    return 1;
-}
-static int rows3(PyObject* const* a, efq_rows_t* r)
-{
-    int64_t shape[3], s[3], t[3];
-    if (a[0] == Py_None) return 0;
-    r->src = ptr(a[0]);
-    r->dst = ptr(a[1]);
-    if (!dims(a[2], shape, 3) || !dims(a[3], s, 3) || !dims(a[4], t, 3)) return -1;
-    r->heads = (int32_t)shape[1];
-    r->src_batch = r->dst_batch = 0;
-    r->src_head = s[1]; r->src_token = s[0];
-    r->dst_head = t[1]; r->dst_token = t[0];
-    return 1;
-}
-/* The cache from (k, v, shape of both, strides of k, of v, page_table, its shape, its strides, cu_seqlens, seq_lens). */
-#define CACHE 10
-static int cache_of(PyObject* const* a, efq_paged_t* c)
-{
-    int64_t shape[4], s[4], t[4], table[2], ts[2];
-    c->k = ptr(a[0]);
-    c->v = ptr(a[1]);
-    if (!dims(a[2], shape, 4) || !dims(a[3], s, 4) || !dims(a[4], t, 4) || !dims(a[6], table, 2) || !dims(a[7], ts, 2)) return 0;
-    if (shape[0] > INT32_MAX || shape[1] > INT32_MAX || shape[2] > INT32_MAX || table[0] > INT32_MAX || table[1] > INT32_MAX) {
-        PyErr_SetString(PyExc_ValueError, "efq_fastcall: the cache has a dimension of more than 32 bits");
-        return 0;
-    }
-    c->n_pages = (int32_t)shape[0]; c->n_heads = (int32_t)shape[1]; c->page_size = (int32_t)shape[2];
-    c->k_page = s[0]; c->k_head = s[1]; c->k_token = s[2];
-    c->v_page = t[0]; c->v_head = t[1]; c->v_token = t[2];
-    c->page_table = ptr(a[5]);
-    c->n_seqs = (int32_t)table[0];
-    c->max_pages = (int32_t)table[1];
-    c->table_stride = ts[0];
-    c->cu_seqlens = ptr(a[8]);
-    c->seq_lens = ptr(a[9]);
-    return !PyErr_Occurred();
-}
-
-/* q rows, k rows, positions, strides of axis and batch, B, S, dtype, rotary, inverse, stream */
-static PyObject* rotary(PyObject* self, PyObject* const* a, Py_ssize_t n)
-{
-    (void)self;
-    if (!want_paged(n, 2 * GROUP + 9)) return NULL;
-    efq_rows_t q = {0}, k = {0};
-    const int has_q = rows4(a, &q), has_k = rows4(a + GROUP, &k);
-    if (has_q < 0 || has_k < 0) return NULL;
-    a += 2 * GROUP;
-    void *positions = ptr(a[0]), *rotation = ptr(a[6]), *stream = ptr(a[8]);
-    const int64_t axis = i64(a[1]), batch = i64(a[2]), S = i64(a[4]);
-    const int B = i32(a[3]), dtype = i32(a[5]), inverse = i32(a[7]);
-    if (PyErr_Occurred()) return NULL;
-    UNLOCKED(efq_status_t, paged_fn.rotary(has_q ? &q : NULL, has_k ? &k : NULL, positions, axis, batch, B, S, 128, dtype, rotation, inverse, stream))
-    return PyLong_FromLong(st);
-}
-
-/* k rows, v rows, q rows, total, positions, stride of axis, cache, dtype, rotary, stream */
-static PyObject* paged_append(PyObject* self, PyObject* const* a, Py_ssize_t n)
-{
-    (void)self;
-    if (!want_paged(n, 3 * GROUP + 3 + CACHE + 3)) return NULL;
-    efq_rows_t k = {0}, v = {0}, q = {0};
-    efq_paged_t cache = {0};
-    const int has_k = rows3(a, &k), has_v = rows3(a + GROUP, &v), has_q = rows3(a + 2 * GROUP, &q);
-    if (has_k < 0 || has_v < 0 || has_q < 0) return NULL;
-    a += 3 * GROUP;
-    const int64_t total = i64(a[0]), axis = i64(a[2]);
-    void* positions = ptr(a[1]);
-    if (!cache_of(a + 3, &cache)) return NULL;
-    a += 3 + CACHE;
-    const int dtype = i32(a[0]);
-    void *rotation = ptr(a[1]), *stream = ptr(a[2]);
-    if (PyErr_Occurred()) return NULL;
-    UNLOCKED(efq_status_t, paged_fn.append(has_k ? &k : NULL, has_v ? &v : NULL, has_q ? &q : NULL, total, positions, axis, &cache, 128, dtype, rotation, stream))
-    return PyLong_FromLong(st);
-}
-
-/* q rows, lse, total, max_seqlen_q, cache, dtype, causal, scale, workspace, bytes, stream */
-static PyObject* paged_attention(PyObject* self, PyObject* const* a, Py_ssize_t n)
-{
-    (void)self;
-    if (!want_paged(n, GROUP + 3 + CACHE + 6)) return NULL;
-    efq_rows_t q = {0};
-    efq_paged_t cache = {0};
-    const int has_q = rows3(a, &q);
-    if (has_q < 0) return NULL;
-    a += GROUP;
-    void* lse = ptr(a[0]);
-    const int64_t total = i64(a[1]);
-    const int max_q = i32(a[2]);
-    if (!cache_of(a + 3, &cache)) return NULL;
-    a += 3 + CACHE;
-    const int dtype = i32(a[0]), causal = i32(a[1]);
-    const float scale = f32(a[2]);
-    void *ws = ptr(a[3]), *stream = ptr(a[5]);
-    const int64_t bytes = i64(a[4]);
-    if (PyErr_Occurred()) return NULL;
-    UNLOCKED(efq_status_t, paged_fn.attention(has_q ? &q : NULL, lse, total, max_q, &cache, 128, dtype, causal, scale, ws, (size_t)bytes, stream))
-    return PyLong_FromLong(st);
-}
-
 static PyMethodDef methods[] = {
     {"set_functions", (PyCFunction)(void (*)(void))set_functions, METH_FASTCALL, NULL},
     {"attention", (PyCFunction)(void (*)(void))attention, METH_FASTCALL, NULL},
@@ -329,10 +178,6 @@ static PyMethodDef methods[] = {
     {"probgen", (PyCFunction)(void (*)(void))probgen, METH_FASTCALL, NULL},
     {"etq_probgen", (PyCFunction)(void (*)(void))etq_probgen, METH_FASTCALL, NULL},
     {"varlen", (PyCFunction)(void (*)(void))varlen, METH_FASTCALL, NULL},
-    {"set_paged_functions", (PyCFunction)(void (*)(void))set_paged_functions, METH_FASTCALL, NULL},
-    {"rotary", (PyCFunction)(void (*)(void))rotary, METH_FASTCALL, NULL},
-    {"paged_append", (PyCFunction)(void (*)(void))paged_append, METH_FASTCALL, NULL},
-    {"paged_attention", (PyCFunction)(void (*)(void))paged_attention, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL},
 };
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "efq_fastcall", NULL, -1, methods, NULL, NULL, NULL, NULL};
