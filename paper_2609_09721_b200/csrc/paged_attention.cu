@@ -245,6 +245,11 @@ efq_status_t paged_attention(const efq_rows_t* q, float* lse, int64_t total, int
     if (total == 0 || cache->n_seqs == 0) return EFQ_OK;
     const int64_t group_rows = static_cast<int64_t>(G) * (max_seqlen_q > 0 ? max_seqlen_q : 1);
     const PagedPlan plan = plan_paged(group_rows);
+    const bool many = plan.rows > kFewRows;
+    const int step = many ? kChunkRows / G * 2 : plan.rows / G;         // new tokens of a query tile
+    if (paged_most_units(total, cache->n_seqs, static_cast<int64_t>(cache->max_pages) * cache->page_size, cache->n_heads, step, many ? kChunkShift : kFewShift,
+                         many ? kChunkItem : kFewItem) >= (1ll << 31))
+        return EFQ_ERR_UNSUPPORTED;
     if (!workspace || workspace_bytes < plan.total) return EFQ_ERR_WORKSPACE;
     if (reinterpret_cast<uintptr_t>(workspace) & 255u) return EFQ_ERR_ALIGNMENT;
     if (!device_is_sm100()) return EFQ_ERR_ARCH;
@@ -279,8 +284,7 @@ efq_status_t paged_attention(const efq_rows_t* q, float* lse, int64_t total, int
     A.part_ml = reinterpret_cast<float2*>(ws + plan.ml);
     A.records = reinterpret_cast<PagedRecord*>(ws + plan.records);
     A.inject_skip_loads = inject_skip_loads ? 1 : 0;
-    const bool many = plan.rows > kFewRows;
-    A.step = many ? kChunkRows / G * 2 : plan.rows / G;
+    A.step = step;
 
     CUtensorMap mq, mk, mv;
     const int keys = many ? kChunkKeys : kFewKeys;

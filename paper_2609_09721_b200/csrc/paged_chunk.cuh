@@ -28,7 +28,7 @@ struct __align__(1024) ChunkSmem {
     uint8_t q[2][2][kChunkPart];                               // half, channels 0-63 and 64-127; 128-byte swizzle
     uint8_t kv[kChunkSlots][2 * kChunkPart];                   // [8 tokens][channels 0-63, 64-127][token]
     uint64_t full[kChunkSlots], empty[kChunkSlots], q_full, q_empty, s_full[2], p_ready[2], p_rest[2], o_full[2], v_tail, v_clean, turn[2], drained[2];
-    int64_t scratch[kChunkThreads / 32];
+    uint32_t scratch[kChunkThreads / 32];
     PagedRun<kChunkShift, kChunkItem> run;
     uint32_t tmem_base;
     volatile uint32_t failed;

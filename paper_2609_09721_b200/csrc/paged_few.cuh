@@ -31,7 +31,7 @@ struct __align__(1024) FewSmem {
     float2 join_ml[kFewWarps][kFewRows];
     float2 row_ml[kFewRows];
     uint64_t full[kStages], empty[kStages], q_full[2], q_empty[2];
-    int64_t scratch[64];
+    uint32_t scratch[kFewThreads / 32];
     PagedRun<kFewShift, kFewItem> run;
     uint32_t bad[kStages];                      // the tile lies on an entry that is no page
     volatile uint32_t failed;
@@ -151,15 +151,6 @@ paged_few_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
         bool ok = true;
         while (ok && walk.next(g)) {
             const uint32_t qb = seg & 1u;
-            if (seg >= 2) ok = paged_wait_warp(&sm->q_empty[qb], ((seg >> 1) - 1) & 1u, sm);
-            if (!ok) break;
-            if (ptx::elect_one()) {
-                ptx::mbar_arrive_expect_tx(&sm->q_full[qb], static_cast<uint32_t>(A.step * A.G) * 256u);
-                tma_load_3d(sm->q[qb][0], &mq, 0, g.head * A.G, g.token0, &sm->q_full[qb]);
-                tma_load_3d(sm->q[qb][1], &mq, 64, g.head * A.G, g.token0, &sm->q_full[qb]);
-            }
-            __syncwarp();
-            ++seg;
             const int32_t* table = A.page_table + g.seq * A.table_stride;
             // as it stands in the table: it is looked at when the tile after the next is loaded, so that nobody waits for it here
             auto entry_of = [&](int j) {
@@ -169,6 +160,15 @@ paged_few_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
                 return e;
             };
             int entry = entry_of(g.j0), next = entry_of(g.j0 + 1);
+            if (seg >= 2) ok = paged_wait_warp(&sm->q_empty[qb], ((seg >> 1) - 1) & 1u, sm);
+            if (!ok) break;
+            if (ptx::elect_one()) {
+                ptx::mbar_arrive_expect_tx(&sm->q_full[qb], static_cast<uint32_t>(A.step * A.G) * 256u);
+                tma_load_3d(sm->q[qb][0], &mq, 0, g.head * A.G, g.token0, &sm->q_full[qb]);
+                tma_load_3d(sm->q[qb][1], &mq, 64, g.head * A.G, g.token0, &sm->q_full[qb]);
+            }
+            __syncwarp();
+            ++seg;
             for (int j = g.j0; j < g.j1; ++j, ++tile) {
                 const int ahead = entry_of(j + 2);
                 const uint32_t stage = tile % kStages;

@@ -18,24 +18,26 @@
 
 namespace efq {
 
-// sum over i < n of floor((b + a i) / 2^shift), a > 0, b >= 0.  The terms grow by a fixed amount from one period of
+// All numbers of units fit 31 bits: a step that might have more is refused (paged_most_units()).  The search for a CTA's run stands before its
+// first load, and it is the instructions that cost there, fetched for the first time; 64 bits made three of one.
+
+// sum over i < n of floor((b + a i) / 2^shift), a > 0, which fits 32 bits.  The terms grow by a fixed amount from one period of
 // 2^shift / gcd(a, 2^shift) terms to the next, so two partial periods are summed term by term and the rest is arithmetic.
-EFQ_HD int64_t paged_floor_sum(int64_t n, int shift, uint32_t a, uint32_t b)
+EFQ_HD uint32_t paged_floor_sum(uint32_t n, int shift, uint32_t a, uint32_t b)
 {
     int low = 0;
     while (low < shift && ((a >> low) & 1u) == 0u) ++low;
     const int period_log = shift - low;
-    const uint32_t period = 1u << period_log;
-    const int64_t full = n >> period_log, grows = static_cast<int64_t>(a) >> low;         // period * a / 2^shift
-    const uint32_t rest = static_cast<uint32_t>(n - (full << period_log)), upto = full > 0 ? period : rest;
-    int64_t of_period = 0, of_rest = 0;
-    uint64_t x = b;
-    for (uint32_t i = 0; i < upto; ++i, x += a) {
+    const uint32_t period = 1u << period_log, full = n >> period_log, rest = n & (period - 1u), grows = a >> low;      // grows = period * a / 2^shift
+    const uint32_t upto = full > 0 ? period : rest;
+    uint32_t of_period = 0, of_rest = 0;
+    for (uint32_t i = 0, x = b; i < upto; ++i, x += a) {
         if (i == rest) of_rest = of_period;
-        of_period += static_cast<int64_t>(x >> shift);
+        of_period += x >> shift;
     }
     if (rest == upto) of_rest = of_period;
-    return full * of_period + grows * static_cast<int64_t>(period) * (full * (full - 1) / 2) + static_cast<int64_t>(rest) * full * grows + of_rest;
+    const uint32_t pairs = full > 0 ? ((full & 1u) != 0u ? (full - 1u) / 2u * full : full / 2u * (full - 1u)) : 0u;
+    return full * of_period + grows * period * pairs + rest * full * grows + of_rest;
 }
 
 // One sequence of the step: lq new tokens in query tiles of `step` tokens, len keys in tiles of 2^kShift.  A query tile costs its key tiles and
@@ -71,26 +73,26 @@ struct SeqWork {
     }
     EFQ_HD int units(int i) const { return key_tiles(i) + kItem; }
     // units of the first n tiles
-    EFQ_HD int64_t units_before(int n) const
+    EFQ_HD int units_before(int n) const
     {
         if (n <= 0) return 0;
-        if (!causal || tiles == 1) return static_cast<int64_t>(n) * units(0);
+        if (!causal || tiles == 1) return n * units(0);
         const int base = len - lq;
         const int blind = base >= 0 ? 0 : -base / step;                         // tiles that see nothing
         const int full = n < tiles ? n : tiles - 1;                             // the last one ends at len and not at a multiple of step
-        int64_t sum = (blind < full ? blind : full) + static_cast<int64_t>(n) * kItem;
-        if (full > blind)
-            sum += paged_floor_sum(full - blind, kShift, static_cast<uint32_t>(step),
-                                   static_cast<uint32_t>(static_cast<int64_t>(base) + static_cast<int64_t>(blind + 1) * step + kKeys - 1));
+        int sum = (blind < full ? blind : full) + n * kItem;
+        if (full > blind)       // blind * step <= lq and base + step <= len + 256: below 2^32 with what is added
+            sum += static_cast<int>(paged_floor_sum(static_cast<uint32_t>(full - blind), kShift, static_cast<uint32_t>(step),
+                                                    static_cast<uint32_t>(base) + static_cast<uint32_t>(blind + 1) * static_cast<uint32_t>(step) + (kKeys - 1u)));
         return n == tiles ? sum + key_tiles(tiles - 1) : sum;
     }
-    EFQ_HD int64_t units_per_head() const { return units_before(tiles); }
+    EFQ_HD int units_per_head() const { return units_before(tiles); }
 };
 
 // The run of units of one CTA, and a walk along it.  Every role of a kernel walks by itself.
 template <int kShift, int kItem>
 struct PagedRun {
-    int64_t left, off;                  // units; the first one's place in its head
+    int32_t left, off;                  // units; the first one's place in its head
     int32_t seq, begin, head, tile, unit;       // where it begins; the sequence's first token in the step
     int32_t begins;                     // CTA that holds unit 0 of that query tile
     SeqWork<kShift, kItem> w;           // of that sequence
@@ -104,49 +106,50 @@ struct PagedSegment {
     int32_t j0, j1, n;                              // key tiles of the run, of the query tile
 };
 
-// Quotients whose operands mostly fit 32 bits
-EFQ_HD uint64_t paged_divide(uint64_t a, uint64_t b)
-{
-    if (((a | b) >> 32) == 0) return static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
-    return a / b;
-}
 // CTA c of `ctas` takes each = total / ctas units, the first `more` CTAs one more (total >= ctas: every CTA has one).
 struct PagedShares {
-    int64_t each, more;
-    EFQ_HD PagedShares(int64_t total, int64_t ctas) : each(static_cast<int64_t>(paged_divide(total, ctas))), more(total - each * ctas) {}
-    EFQ_HD int64_t first(int64_t c) const { return each * c + (c < more ? c : more); }
-    EFQ_HD int64_t units(int64_t c) const { return each + (c < more ? 1 : 0); }
-    EFQ_HD int64_t cta_of(int64_t unit) const
+    uint32_t each, more;
+    EFQ_HD PagedShares(uint32_t total, uint32_t ctas) : each(total / ctas), more(total - each * ctas) {}
+    EFQ_HD uint32_t first(uint32_t c) const { return each * c + (c < more ? c : more); }
+    EFQ_HD uint32_t units(uint32_t c) const { return each + (c < more ? 1u : 0u); }
+    EFQ_HD uint32_t cta_of(uint32_t unit) const
     {
-        const int64_t wide = (each + 1) * more;
-        return static_cast<int64_t>(unit < wide ? paged_divide(unit, each + 1) : more + paged_divide(unit - wide, each));
+        const uint32_t wide = (each + 1u) * more;
+        return unit < wide ? unit / (each + 1u) : more + (unit - wide) / each;
     }
 };
+// More units than a step can have: `tokens` new ones in n_seqs sequences of at most `keys` keys.
+EFQ_HD int64_t paged_most_units(int64_t tokens, int n_seqs, int64_t keys, int heads, int step, int shift, int item)
+{
+    const int64_t tiles = tokens / step + n_seqs, of_tile = (keys >> shift) + 1 + item;
+    return tiles > (int64_t{1} << 40) / of_tile ? int64_t{1} << 62 : tiles * of_tile * heads;
+}
 // The run of CTA c, which begins at unit `off` of sequence s; paged_begin_tile() has to follow with the query tile that holds unit run->unit of
 // the head.
 template <int kShift, int kItem>
-EFQ_HD void paged_begin_run(const SeqWork<kShift, kItem>& w, int s, int begin, int64_t per_head, int64_t off, const PagedShares& shares, int64_t c,
+EFQ_HD void paged_begin_run(const SeqWork<kShift, kItem>& w, int s, int begin, uint32_t per_head, uint32_t off, const PagedShares& shares, uint32_t c,
                             PagedRun<kShift, kItem>* run)
 {
-    run->left = shares.units(c);
+    run->left = static_cast<int32_t>(shares.units(c));
     run->seq = s;
     run->begin = begin;
     run->w = w;
-    run->head = static_cast<int32_t>(paged_divide(off, per_head));
-    run->off = off - run->head * per_head;
+    const uint32_t head = off / per_head;
+    run->head = static_cast<int32_t>(head);
+    run->off = static_cast<int32_t>(off - head * per_head);
     run->tile = 0;
     run->unit = 0;
     run->begins = static_cast<int32_t>(c);
 }
 // Whether query tile `tile` holds the run's first unit; if so, the run begins there.
 template <int kShift, int kItem>
-EFQ_HD bool paged_begin_tile(int tile, const PagedShares& shares, int64_t c, PagedRun<kShift, kItem>* run)
+EFQ_HD bool paged_begin_tile(int tile, const PagedShares& shares, uint32_t c, PagedRun<kShift, kItem>* run)
 {
-    const int64_t unit = run->off - run->w.units_before(tile);
+    const int unit = run->off - run->w.units_before(tile);
     if (unit < 0 || unit >= run->w.units(tile)) return false;
     run->tile = tile;
-    run->unit = static_cast<int32_t>(unit);
-    run->begins = static_cast<int32_t>(shares.cta_of(shares.first(c) - unit));
+    run->unit = unit;
+    run->begins = static_cast<int32_t>(shares.cta_of(shares.first(c) - static_cast<uint32_t>(unit)));
     return true;
 }
 
@@ -154,8 +157,7 @@ EFQ_HD bool paged_begin_tile(int tile, const PagedShares& shares, int64_t c, Pag
 template <int kShift, int kItem, typename Read>
 struct PagedWalk {
     Read read;
-    int n_seqs, heads;
-    int64_t left;
+    int n_seqs, heads, left;
     int seq, head, tile, unit, begin;
     SeqWork<kShift, kItem> w;
 
@@ -181,7 +183,7 @@ struct PagedWalk {
                 }
             }
             const int first = tile * w.step, n = w.key_tiles(tile), from = unit, all = n + kItem - from;
-            const int taken = all < left ? all : static_cast<int>(left);
+            const int taken = all < left ? all : left;
             left -= taken;
             unit = 0;
             ++tile;

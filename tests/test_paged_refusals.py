@@ -45,6 +45,7 @@ def test_attention_refuses():
     assert _attention(R, K, d=64) == UNSUPPORTED and _attention(R, K, dtype=2) == UNSUPPORTED
     assert _attention(_rows(heads=258), K) == UNSUPPORTED                             # 129 query heads on a KV head
     assert _attention(R, K, total=1 << 31) == UNSUPPORTED
+    assert _attention(R, _cache(max_pages=1 << 26, n_seqs=600)) == UNSUPPORTED           # may have 2^31 key tiles
     for bad in (dict(src=P + 8), dict(dst=P + 2), dict(src_head=100), dict(src_token=4), dict(dst_head=12)):
         assert _attention(_rows(**bad), K) == ALIGNMENT, bad
     for bad in (dict(k=P + 8), dict(v=P + 4), dict(k_page=4), dict(v_head=100), dict(k_token=132)):

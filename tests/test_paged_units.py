@@ -33,22 +33,23 @@ int64_t all_segments(const int32_t* cu, const int32_t* lens, int n_seqs, int hea
 {
     const Reader<kShift, kItem> read{cu, lens, step, causal};
     efq::SeqWork<kShift, kItem> w;
-    int64_t total = 0, n = 0;
+    uint32_t total = 0;
+    int64_t n = 0;
     int b;
     for (int s = 0; s < n_seqs; ++s) {
         read(s, w, b);
         total += w.units_per_head() * heads;
     }
-    const int64_t ctas = grid < total ? grid : total;
+    const uint32_t ctas = (uint32_t)grid < total ? grid : total;
     if (total == 0) return 0;
     const efq::PagedShares shares(total, ctas);
-    for (int64_t c = 0; c < ctas; ++c) {
+    for (uint32_t c = 0; c < ctas; ++c) {
         efq::PagedRun<kShift, kItem> run{};
-        int64_t off = shares.first(c);
+        uint32_t off = shares.first(c);
         if (shares.cta_of(off) != c) return -2;
         for (int s = 0; s < n_seqs; ++s) {
             read(s, w, b);
-            const int64_t per_head = w.units_per_head();
+            const uint32_t per_head = w.units_per_head();
             if (off < per_head * heads) { efq::paged_begin_run(w, s, b, per_head, off, shares, c, &run); break; }
             off -= per_head * heads;
         }
@@ -109,10 +110,10 @@ def test_units_in_closed_form(lib):
 
 
 def test_units_of_the_longest_sequences(lib):
-    """A whole prompt of two million tokens, and the last tile before 2^31 keys: the sums stay exact in 64 bits."""
-    lq = len_ = 2_000_003
-    for step in (64, 50, 1):
-        assert lib.before(lq, len_, step, 128, 0, 1, -(-lq // step)) == sum(_units(lq, len_, step, 128, 1))
+    """Whole prompts of millions of tokens up to the 2^31 units that a step may have, and the last tile before 2^31 keys."""
+    for lq, step in ((2_000_003, 64), (2_000_003, 50), (500_000, 1), (5_000_000, 256)):
+        want = _units(lq, lq, step, 128, 1)
+        assert sum(want) < 2**31 and lib.before(lq, lq, step, 128, 0, 1, len(want)) == sum(want)
     assert lib.before(1, 2**31 - 1, 16, 64, 0, 1, 1) == 2**25
     assert lib.before(200, 2**31 - 1, 64, 128, 0, 1, 4) == sum(_units(200, 2**31 - 1, 64, 128, 1))
 
