@@ -27,7 +27,7 @@ constexpr float kSlack = 8.0f;                                 // log2: probabil
 struct __align__(1024) ChunkSmem {
     uint8_t q[2][2][kChunkPart];                               // half, channels 0-63 and 64-127; 128-byte swizzle
     uint8_t kv[kChunkSlots][2 * kChunkPart];                   // [8 tokens][channels 0-63, 64-127][token]
-    uint64_t full[kChunkSlots], empty[kChunkSlots], q_full, q_empty, s_full[2], p_ready[2], p_rest[2], o_full[2], v_tail, v_clean, turn[2], drained[2];
+    uint64_t full[kChunkSlots], empty[kChunkSlots], q_full, q_empty, s_full[2], p_ready[2], p_rest[2], o_full[2], v_tail, v_clean, drained[2];
     uint32_t scratch[kChunkThreads / 32];
     PagedRun<kChunkShift, kChunkItem> run;
     uint32_t tmem_base;
@@ -134,11 +134,10 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
         ptx::mbar_init(&sm->v_clean, 1);
         for (int i = 0; i < 2; ++i) {
             ptx::mbar_init(&sm->s_full[i], 1);
-            ptx::mbar_init(&sm->p_ready[i], 4);
+            ptx::mbar_init(&sm->p_ready[i], 5);
             ptx::mbar_init(&sm->p_rest[i], 4);
             ptx::mbar_init(&sm->o_full[i], 1);
             ptx::mbar_init(&sm->drained[i], 1);
-            ptx::mbar_init(&sm->turn[i], 1);
         }
         ptx::mbar_init_fence();
         ptx::prefetch_tensormap(&mq);
@@ -234,9 +233,10 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
             const uint64_t dv = ptx::smem_desc(ptx::smem_u32(sm->kv[0]), 1024, 2048, ptx::kLayoutSw128);
             constexpr uint32_t kSlotStep = 2 * kChunkPart >> 4;
             uint64_t *const s_full = &sm->s_full[w], *const p_ready = &sm->p_ready[w], *const p_rest = &sm->p_rest[w], *const o_full = &sm->o_full[w];
-            uint64_t *const turn_mine = &sm->turn[w], *const turn_other = &sm->turn[w ^ 1];
-            uint32_t slot = 0, round = 0, q_round = 0, p_round = 0, clean_round = 0, turn_round = 0;        // parities of the next waits
-            bool ok = true, first = w == 0;         // nobody is before the first half's first turn
+            uint64_t* const p_ready_other = &sm->p_ready[w ^ 1];
+            uint32_t slot = 0, round = 0, q_round = 0, p_round = 0, clean_round = 0;        // parities of the next waits
+            uint32_t turns = 0;                  // given to the other half
+            bool ok = true;
             auto advance = [&]() {
                 if (++slot == kChunkSlots) {
                     slot = 0;
@@ -244,48 +244,44 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
                 }
             };
             // The halves take turns, the first one first: while one has its products the other has its softmax.  Left to themselves they fall
-            // into step, both at the exponentials and then both at the tensor core.
-            auto my_turn = [&]() {
-                if (first) {
-                    first = false;
-                    return true;
-                }
-                const bool there = paged_wait_warp(turn_mine, turn_round, sm);
-                turn_round ^= 1u;
-                return there;
-            };
+            // into step, both at the exponentials and then both at the tensor core.  A half's turn for a tile is an arrival of the other
+            // half's warp on the barrier of its probabilities, so that there is one wait for both.  Half 0 gives half 1 the turn for the same
+            // tile, half 1 half 0 that for the next.
+            // The barrier takes one turn a phase: a warp that does not wait for its own half's probabilities waits until the last one has been taken.
+            auto turn_taken = [&]() { return turns == 0u || paged_wait_warp(p_ready_other, (turns & 1u) ^ 1u, sm); };
             // one thread's; hands over before the last products, which the queue holds until the other warp is there
-            auto scores = [&]() {
+            auto scores = [&](bool hand_over) {
                 const uint64_t k = dk + slot * kSlotStep;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const uint32_t off = ((i >> 2) * kChunkPart + (i & 3) * 32) >> 4, k_off = ((i >> 2) * 1024 + (i & 3) * 32) >> 4;
                     ptx::mma_bf16(s_tmem, dq + off, k + k_off, chunk_idesc<T>(false), i > 0 ? 1u : 0u);
-                    if (i == 4) ptx::mbar_arrive(turn_other);
+                    if (i == 4 && hand_over) ptx::mbar_arrive(p_ready_other);
                 }
                 ptx::mma_commit(s_full);
                 ptx::mma_commit(&sm->empty[slot]);
             };
             while (ok && walk.next(g)) {
                 const int e0 = chunk_half(g, 0, A.step).end, e1 = chunk_half(g, 1, A.step).end;
-                const int j0 = uniform(g.j0), mine = uniform(w ? e1 : e0), end = uniform(max(e0, e1)), clean = uniform(g.w.len < max(e0, e1) * kChunkKeys ? 1 : 0);
+                const int j0 = uniform(g.j0), mine = uniform(w ? e1 : e0), other = uniform(w ? e0 : e1), end = uniform(max(e0, e1)), clean = uniform(g.w.len < max(e0, e1) * kChunkKeys ? 1 : 0);
                 if (end == j0) continue;
                 ok = paged_wait_warp(&sm->q_full, q_round, sm) && paged_wait_warp(&sm->full[slot], round, sm);
                 q_round ^= 1u;
-                if (!ok) break;
-                // the first scores
-                ok = my_turn();
+                // the first scores; half 1 gives half 0 the turn for the first tile
+                const bool opens = w == 1 && j0 < other;
+                if (opens) ok = ok && turn_taken();
                 if (!ok) break;
                 if (ptx::elect_one()) {
                     if (j0 < mine) {
-                        scores();
+                        scores(opens);
                     } else {
-                        ptx::mbar_arrive(turn_other);
+                        if (opens) ptx::mbar_arrive(p_ready_other);
                         ptx::mbar_arrive(&sm->empty[slot]);
                     }
                     if (j0 + 1 == end) ptx::mma_commit(&sm->q_empty);
                 }
                 __syncwarp();
+                turns += opens ? 1u : 0u;
                 advance();
                 for (int j = j0; j < end; ++j) {
                     const uint32_t v_slot = slot;
@@ -297,11 +293,11 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
                         ok = ok && paged_wait_warp(&sm->v_clean, clean_round, sm);
                         clean_round ^= 1u;
                     }
-                    const bool more = j + 1 < end;
+                    const bool more = j + 1 < end, hand_over = j + w < other;          // w = 0: tile j of the other half, w = 1: tile j + 1
                     if (more) ok = ok && paged_wait_warp(&sm->full[slot], round, sm);
                     if (j < mine) {
                         const uint64_t v = dv + v_slot * kSlotStep;
-                        ok = ok && paged_wait_warp(p_ready, p_round, sm) && my_turn();
+                        ok = ok && paged_wait_warp(p_ready, p_round, sm);
                         if (!ok) break;
                         ptx::tc_fence_after_sync();
                         if (ptx::elect_one()) {
@@ -318,10 +314,10 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
 #pragma unroll
                             for (int i = 6; i < 8; ++i) ptx::mma_bf16_ts(o_tmem, s_tmem + 8 * i, v + (i * 4096u >> 4), chunk_idesc<T>(true), 1u);
                             if (j + 1 < mine) {
-                                scores();
+                                scores(hand_over);
                             } else {
                                 ptx::mma_commit(o_full);
-                                ptx::mbar_arrive(turn_other);
+                                if (hand_over) ptx::mbar_arrive(p_ready_other);
                                 if (more) ptx::mbar_arrive(&sm->empty[slot]);
                             }
                             ptx::mma_commit(&sm->empty[v_slot]);
@@ -329,16 +325,17 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
                         }
                         __syncwarp();
                     } else {
-                        ok = ok && my_turn();
+                        if (hand_over) ok = ok && turn_taken();
                         if (!ok) break;
                         if (ptx::elect_one()) {
-                            ptx::mbar_arrive(turn_other);
+                            if (hand_over) ptx::mbar_arrive(p_ready_other);
                             ptx::mbar_arrive(&sm->empty[v_slot]);
                             if (more) ptx::mbar_arrive(&sm->empty[slot]);
                             if (j + 2 == end) ptx::mma_commit(&sm->q_empty);
                         }
                         __syncwarp();
                     }
+                    turns += hand_over ? 1u : 0u;
                     if (more) advance();
                 }
             }
