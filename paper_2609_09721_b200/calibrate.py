@@ -5,7 +5,8 @@
 Runs the fused EFQ forward for every candidate pair on the seeded inputs of the workload, measures
 rho = ||O~ - O_ref||_F / ||O_ref||_F against FP32 attention on the unquantised inputs, prints the surface and
 the pair with the smallest rho.  Real calibration activations are the caller's business: this tool takes the
-shapes and value distributions of the synthetic workloads, nothing else.
+shapes and value distributions of the synthetic workloads, nothing else.  With --rotary their q and k carry the tokens' positions, as a
+model's do when they reach the attention (a text's running index, a video's time, height and width).
 """
 from __future__ import annotations
 
@@ -30,10 +31,16 @@ def _grid(spec: str):
     return [round(lo + i * step, 6) for i in range(n)]
 
 
-def surface(case, taus, hs):
+def surface(case, taus, hs, rotary=False):
     qb, kb, vb = inputs.make_qkv(case)
     dev = lambda a: torch.from_numpy(a.view(np.int16)).cuda().view(torch.bfloat16)
     q, k, v = dev(qb), dev(kb), dev(vb)
+    if rotary:
+        r = inputs.rotary_recipe(case)
+        turn = binding.Rotary.of(r.sections, r.theta, r.interleaved, r.ladder_per_axis)
+        positions = torch.from_numpy(r.positions).cuda()
+        binding.efq_rotary(q, None, positions[:, case.Sk - case.Sq:], turn, q_out=q)      # queries are the last tokens
+        binding.efq_rotary(None, k, positions, turn, k_out=k)
     o_ref = binding.efq_exact_attention_fwd(q, k, v, case.causal)
     table, best = binding.efq_calibrate(q, k, v, o_ref, taus, hs, case.causal)
     return np.array(table), best
@@ -44,17 +51,18 @@ def main(argv=None):
     ap.add_argument("--workload", default="qwen3_8b_2k", choices=sorted(WORKLOADS))
     ap.add_argument("--tau", default="-3.6:-1.8:0.3", help="lo:hi:step")
     ap.add_argument("--h", default="1.6:3.0:0.2", help="lo:hi:step")
+    ap.add_argument("--rotary", action="store_true", help="turn the tokens' positions into q and k first")
     args = ap.parse_args(argv)
     taus, hs = _grid(args.tau), _grid(args.h)
     case = WORKLOADS[args.workload]()
-    rho, best = surface(case, taus, hs)
-    print(f"workload {case.name}: rho(tau, h) = ||O~ - O_ref||_F / ||O_ref||_F, rows tau, columns h")
+    rho, best = surface(case, taus, hs, args.rotary)
+    print(f"workload {case.name}{' with rotary positions' if args.rotary else ''}: rho(tau, h) = ||O~ - O_ref||_F / ||O_ref||_F, rows tau, columns h")
     print("tau\\h   " + " ".join(f"{h:7.2f}" for h in hs))
     for t, row in zip(taus, rho):
         print(f"{t:6.2f}  " + " ".join(f"{x:7.4f}" for x in row))
     print(f"selected (tau, h) = ({best[0]:.2f}, {best[1]:.2f}), rho = {rho.min():.4f}")
     for name, (t, h) in (("EFQ-Mean", (-3.06, 2.30)), ("EFQ-MMLU", (-2.90, 2.00)), ("EFQ-Balance", (-2.10, 2.70))):
-        r, _ = surface(case, [t], [h])
+        r, _ = surface(case, [t], [h], args.rotary)
         print(f"{name:12s} ({t:.2f}, {h:.2f}): rho = {r[0, 0]:.4f}")
     return 0
 

@@ -173,6 +173,25 @@ def make_qkv(case: AttentionCase):
     return q, k, v
 
 
+@dataclass(frozen=True)
+class RotaryRecipe:
+    sections: tuple          # pairs of channels of each axis
+    theta: float
+    interleaved: bool
+    ladder_per_axis: bool
+    positions: np.ndarray    # int32 [axes, S]
+
+
+def rotary_recipe(case: AttentionCase, first: int = 0) -> RotaryRecipe:
+    """Positions of a workload's tokens and how its model turns them into q and k: a video's in time, height and width (latent
+    frames of 30 x 52, each axis with a ladder of frequencies of its own, neighbouring channels paired), a text's running index
+    from `first` on (channels p and p + 64 paired)."""
+    t = np.arange(case.Sk, dtype=np.int32) + np.int32(first)
+    if case.recipe == "lowrank":
+        return RotaryRecipe((22, 21, 21), 1e4, True, True, np.stack([t // 1560, t // 52 % 30, t % 52]).astype(np.int32))
+    return RotaryRecipe((64,), 1e6, False, False, t[None].copy())
+
+
 def make_score_matrix(rows: int = 4096, cols: int = 16384, seed: int = 2,
                       sigma: float = 3.0, spike: float = 12.0, spike_frac: float = 0.01):
     """Standalone-stage workload: fp32 scores N(0, sigma^2) with a seeded 1 % of the entries

@@ -213,3 +213,29 @@ def test_recorded_into_a_graph():
         assert torch.equal(want, q_out) and torch.equal(vc.view(torch.int16), p.d_v_cache.view(torch.int16))
         at = (int(p.table[1, (199 - back) // 16]), slice(None), (199 - back) % 16)
         assert torch.equal(p.d_v_cache[at], v[1])
+
+
+@pytest.mark.parametrize("workload", ["single", "video"])
+def test_calibration_on_rotated_workloads(workload, capsys):
+    """The tool's --rotary turns the workload's q and k as the formula does: its surface is that of the inputs turned in 64 bits, up to
+    what a rounding of q and k that falls the other way may change (a few elements in ten thousand, each by a step of 2^-8)."""
+    import numpy as np
+
+    from paper_2609_09721_b200 import calibrate, inputs
+    case = inputs.case_single_head(512, 1) if workload == "single" else inputs.case_wan22(1600, seed=5, H=2)
+    taus, hs = [-3.06, -2.1], [2.3]
+    got, best = calibrate.surface(case, taus, hs, rotary=True)
+    r = inputs.rotary_recipe(case)
+    assert r.positions.shape == (len(r.sections), case.Sk)
+    if workload == "video":
+        assert r.positions[:, 0].tolist() == [0, 0, 0] and r.positions[:, 1599].tolist() == [1, 0, 39]
+    turn = binding.Rotary.of(r.sections, r.theta, r.interleaved, r.ladder_per_axis)
+    q, k, v = (torch.from_numpy(x.view(np.int16)).cuda().view(torch.bfloat16) for x in inputs.make_qkv(case))
+    pos = torch.from_numpy(r.positions).cuda()
+    q, k = (rotate(x, pos, turn.inv_freq, r.sections, r.interleaved).to(torch.bfloat16) for x in (q, k))
+    want, want_best = binding.efq_calibrate(q, k, v, binding.efq_exact_attention_fwd(q, k, v, case.causal), taus, hs, case.causal)
+    assert np.allclose(got, np.array(want), rtol=1e-3) and best == want_best
+    plain, _ = calibrate.surface(case, taus, hs)
+    assert not np.allclose(got, plain, rtol=1e-3)               # the positions matter
+    assert calibrate.main(["--workload", "single_head_1024", "--tau=-3.0:-2.7:0.3", "--h", "2.0:2.0:0.2", "--rotary"]) == 0
+    assert "with rotary positions" in capsys.readouterr().out
