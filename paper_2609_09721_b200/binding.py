@@ -493,15 +493,26 @@ class Rotary:
         return cls(torch.tensor([float(theta) ** -x for x in steps], dtype=torch.float64, device=device or "cuda"), sections, interleaved)
 
 
-def _out(x, out):
-    return torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None and x is not None else out
+def _new(shape, dtype, device, stream):
+    """A tensor that belongs to the stream of the call: memory that the current stream may still be using, or may be given next, is no
+    place for what another one writes."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(int(stream)) if int(stream) != 0 else torch.cuda.default_stream()
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _out(x, out, stream):
+    return _new(x.shape, x.dtype, x.device, stream) if out is None and x is not None else out
 
 
 def efq_rotary(q, k, positions, rotary: Rotary, inverse: bool = False, q_out=None, k_out=None, stream=None):
     """Rotary positions turned into q [B, Hq, S, 128] and k [B, Hkv, S, 128] (bf16 or fp16, any strides; either may be None) in one
     launch.  positions: int32 [axes, S], or [axes, B, S].  q_out and k_out: the outputs (q and k themselves: in place); new tensors are
     contiguous, as the forwards take them.  inverse: turned back, which is the gradient.  Returns (q_out, k_out)."""
-    q_out, k_out = _out(q, q_out), _out(k, k_out)
+    q_out, k_out = _out(q, q_out, stream), _out(k, k_out, stream)
     st = (_tensors or _tensorcall()).rotary(q, k, positions, rotary.address_on(_raw_device()), 1 if inverse else 0, q_out, k_out, _raw_device(), _stream(stream))
     if st:
         _check(st, "efq_rotary")
@@ -514,7 +525,7 @@ def efq_paged_append(k, v, k_cache, v_cache, page_table, cu_seqlens, seq_lens, r
     rotates q [total, Hq, 128] beside them.  cu_seqlens [n_seqs + 1], seq_lens [n_seqs], page_table [n_seqs, max_pages]: int32 CUDA tensors;
     seq_lens counts the new tokens too.  positions: int32 [axes, total], None: a token's index in its sequence.  Returns q_out, or None
     without q."""
-    q_out = _out(q, q_out)
+    q_out = _out(q, q_out, stream)
     device = _raw_device()
     st = (_tensors or _tensorcall()).paged_append(k, v, k_cache, v_cache, page_table, cu_seqlens, seq_lens, None if rotary is None else rotary.address_on(device),
                                                   positions, q, q_out, device, _stream(stream))
@@ -527,18 +538,18 @@ def efq_paged_attention_workspace_bytes(Hq: int, Hkv: int, max_seqlen_q: int, d:
     return int(lib().efq_paged_attention_workspace_bytes(Hq, Hkv, max_seqlen_q, d))
 
 
-def _paged_workspace(q, k_cache, max_seqlen_q):
+def _paged_workspace(q, k_cache, max_seqlen_q, stream):
     n = efq_paged_attention_workspace_bytes(q.shape[1], k_cache.shape[1], max_seqlen_q, q.shape[2]) if q.dim() == 3 and k_cache.dim() == 4 else 0
-    return torch.empty(max(n, 256), dtype=torch.uint8, device=q.device)
+    return _new(max(n, 256), torch.uint8, q.device, stream)
 
 
 def efq_paged_attention_fwd(q, k_cache, v_cache, page_table, cu_seqlens, seq_lens, max_seqlen_q: int, causal: bool = True,
                             softmax_scale: float = 0.0, o=None, lse=None, workspace=None, stream=None):
     """Softmax attention of a step's new tokens q [total, Hq, 128] over a paged cache [pages, Hkv, page_size, 128] (tables as for
     efq_paged_append); max_seqlen_q: the most new tokens of any sequence.  lse: optional fp32 [total, Hq] output.  Returns o, of q's type."""
-    o = _out(q, o)
+    o = _out(q, o, stream)
     if workspace is None:
-        workspace = _paged_workspace(q, k_cache, max_seqlen_q)
+        workspace = _paged_workspace(q, k_cache, max_seqlen_q, stream)
     st = (_tensors or _tensorcall()).paged_attention(q, k_cache, v_cache, page_table, cu_seqlens, seq_lens, max_seqlen_q, 1 if causal else 0, softmax_scale, o, lse,
                                                      workspace, _raw_device(), _stream(stream))
     if st:

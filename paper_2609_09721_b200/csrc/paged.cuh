@@ -37,7 +37,7 @@ inline bool aligned_rows(const void* p, int64_t a, int64_t b, int64_t c) { retur
 // The cache's own fields; the tables' contents are looked at by the kernels.
 inline efq_status_t check_paged(const efq_paged_t& c, int d, int dtype)
 {
-    if (!c.k || !c.v || !c.page_table || !c.cu_seqlens || !c.seq_lens) return EFQ_ERR_INVALID_ARG;
+    if (!c.k || !c.v || (c.n_seqs > 0 && (!c.page_table || !c.cu_seqlens || !c.seq_lens))) return EFQ_ERR_INVALID_ARG;
     if (c.n_pages <= 0 || c.n_heads <= 0 || c.max_pages <= 0 || c.n_seqs < 0 || c.table_stride < 0) return EFQ_ERR_INVALID_ARG;
     if (dtype != EFQ_BF16 && dtype != EFQ_FP16) return EFQ_ERR_UNSUPPORTED;
     if (d != kPagedD || c.page_size < 16 || c.page_size > 4096 || (c.page_size & (c.page_size - 1)) != 0) return EFQ_ERR_UNSUPPORTED;

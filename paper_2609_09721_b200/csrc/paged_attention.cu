@@ -232,7 +232,8 @@ cudaError_t launch_chunk(const CUtensorMap& mq, const CUtensorMap& mk, const CUt
 efq_status_t paged_attention(const efq_rows_t* q, float* lse, int64_t total, int max_seqlen_q, const efq_paged_t* cache, int d, int dtype, int causal,
                              float softmax_scale, void* workspace, size_t workspace_bytes, void* stream, bool inject_skip_loads)
 {
-    if (!q || !cache || !q->src || !q->dst || total < 0 || max_seqlen_q < 0 || q->heads <= 0) return EFQ_ERR_INVALID_ARG;
+    if (!q || !cache || total < 0 || max_seqlen_q < 0 || q->heads <= 0) return EFQ_ERR_INVALID_ARG;
+    if (total > 0 && (!q->src || !q->dst)) return EFQ_ERR_INVALID_ARG;
     if (!(softmax_scale == softmax_scale) || softmax_scale > 3.0e38f) return EFQ_ERR_INVALID_ARG;
     const efq_status_t st = check_paged(*cache, d, dtype);
     if (st != EFQ_OK) return st;

@@ -1,6 +1,7 @@
 """efq_paged_attention_fwd against softmax attention in 64 bits: query rows of a KV group from one to many, lengths around the tiles and
 pages, every type and layout, steps of many sequences, and what must not matter (stale pages, unused entries, other rows)."""
 import math
+import random
 
 import pytest
 import torch
@@ -187,3 +188,68 @@ def test_on_a_side_stream():
         binding.efq_paged_attention_fwd(p.d_q, p.d_k_cache, p.d_v_cache, *p.tables, 60, o=o, workspace=workspace, stream=s)
     s.synchronize()
     assert torch.equal(o, want)
+
+
+@pytest.mark.parametrize("seed", range(48))
+def test_drawn_steps(seed):
+    """Steps of every kind drawn at random: decode, drafts, chunks and mixtures, heads, pages, types, layouts, masks."""
+    rng = random.Random(seed)
+    Hkv = rng.choice([1, 2, 3, 8])
+    G = rng.choice([1, 2, 3, 4, 5, 7, 8, 12, 16, 24, 48])
+    kind = rng.choice(["decode", "draft", "chunk", "mixed"])
+    n = rng.choice([1, 2, 5, 17, 60])
+    top = {"decode": 1, "draft": 7, "chunk": 700, "mixed": 90}[kind]
+    lens = []
+    for _ in range(n if kind != "chunk" else min(n, 2)):
+        a = rng.choice([0, 1, top, rng.randint(1, top)])
+        lens.append((a, rng.choice([a, max(a - 3, 0), a + rng.randint(0, 40), a + rng.randint(0, 3000)])))
+    p = Paged(lens, Hkv * G, Hkv, rng.choice([16, 32, 64, 128, 256]), rng.choice([torch.bfloat16, torch.bfloat16, torch.float16]), seed, hot=rng.choice([0, 8]),
+              token_major=rng.random() < 0.4, tail=rng.choice([0, 3]), slack=rng.choice([1, 5]))
+    causal = rng.random() < 0.7
+    if p.total:
+        _check(p, *_run(p, causal), causal)
+
+
+@pytest.mark.parametrize("n", [1, 40])
+def test_a_cache_of_more_than_32_bits(n):
+    """Pages whose elements lie past 2^31 from the cache's start, written by the append and read by the attention."""
+    Hq, Hkv, page, pages = 8, 4, 64, 70000
+    cache = [torch.empty(pages, Hkv, page, D, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    assert cache[0].numel() > 2**31
+    ids = torch.tensor([[pages - 1, 65600, 3, pages - 2, 66000, -1]], dtype=torch.int32, device="cuda")
+    p = Paged([(n, 300)], Hq, Hkv, page, seed=13)
+    for c in cache:
+        c[ids[0, :5].long()] = math.nan
+    cu, lens = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([0, 300], [300]))
+    binding.efq_paged_append(p.k[0].cuda(), p.v[0].cuda(), *cache, ids, cu, lens)
+    o = binding.efq_paged_attention_fwd(p.d_q, *cache, ids, p.d_cu, p.d_seq_lens, n)
+    _check(p, o, None)
+    assert torch.equal(cache[1][65600, :, 5], p.v[0][69].cuda())
+
+
+def test_two_streams_at_once():
+    """Calls that overlap, each with outputs and a workspace of its own (made by the binding on the call's stream): the same bits as alone."""
+    ps = [Paged([(1, 5000), (1, 300)], 8, 2, 16, seed=14), Paged([(130, 2000), (7, 900)], 8, 2, 32, seed=15)]
+    want = [_run(p, lse=False)[0] for p in ps]
+    streams = [torch.cuda.Stream() for _ in ps]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(20):
+        for p, s, g in zip(ps, streams, got):
+            g.append(binding.efq_paged_attention_fwd(p.d_q, p.d_k_cache, p.d_v_cache, *p.tables, p.max_q, stream=s))
+    torch.cuda.synchronize()
+    for w, g in zip(want, got):
+        assert all(torch.equal(w, x) for x in g)
+
+
+def test_nothing_to_do():
+    p = Paged([(3, 30)], 4, 2, 16, seed=16)
+    o = binding.efq_paged_attention_fwd(p.d_q[:0], p.d_k_cache, p.d_v_cache, p.d_table, torch.zeros(2, dtype=torch.int32, device="cuda"), p.d_seq_lens, 0)
+    assert o.shape == (0, 4, D)
+    none = torch.zeros(0, dtype=torch.int32, device="cuda")
+    o = torch.full_like(p.d_q, 7.0)
+    binding.efq_paged_attention_fwd(p.d_q, p.d_k_cache, p.d_v_cache, p.d_table[:0], torch.zeros(1, dtype=torch.int32, device="cuda"), none, 3, o=o)
+    assert (o == 7.0).all()
+    for cu in ([0, 0], [5, 2], [-3, 1], [2, 9]):                 # no new tokens, and prefix sums that are none of the step's: nothing is written
+        binding.efq_paged_attention_fwd(p.d_q, p.d_k_cache, p.d_v_cache, p.d_table, torch.tensor(cu, dtype=torch.int32, device="cuda"), p.d_seq_lens, 3, o=o)
+        assert (o == 7.0).all(), cu

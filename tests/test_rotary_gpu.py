@@ -239,3 +239,21 @@ def test_calibration_on_rotated_workloads(workload, capsys):
     assert not np.allclose(got, plain, rtol=1e-3)               # the positions matter
     assert calibrate.main(["--workload", "single_head_1024", "--tau=-3.0:-2.7:0.3", "--h", "2.0:2.0:0.2", "--rotary"]) == 0
     assert "with rotary positions" in capsys.readouterr().out
+
+
+def test_nothing_to_do():
+    r = _rotary((64,), False, False)
+    pos = torch.zeros(1, 0, dtype=torch.int32, device="cuda")
+    x = torch.zeros(2, 4, 0, D, dtype=torch.bfloat16, device="cuda")
+    assert binding.efq_rotary(x, x, pos, r)[1].shape == x.shape
+    x = torch.zeros(0, 4, 3, D, dtype=torch.bfloat16, device="cuda")
+    assert binding.efq_rotary(x, None, torch.zeros(1, 3, dtype=torch.int32, device="cuda"), r)[0].shape == x.shape
+    p = Paged([(3, 30)], 4, 2, 16, seed=16)
+    k = torch.ones(3, 2, D, device="cuda").bfloat16()
+    before = p.d_v_cache.clone()
+    q = torch.full_like(p.d_q, 7.0)
+    none, zero = torch.zeros(0, dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    binding.efq_paged_append(k[:0], k[:0], p.d_k_cache, p.d_v_cache, p.d_table, torch.zeros(2, dtype=torch.int32, device="cuda"), p.d_seq_lens, r, None, p.d_q[:0])
+    binding.efq_paged_append(k, k, p.d_k_cache, p.d_v_cache, p.d_table[:0], zero, none, r, None, p.d_q, q)
+    binding.efq_paged_append(k, k, p.d_k_cache, p.d_v_cache, p.d_table, torch.zeros(2, dtype=torch.int32, device="cuda"), p.d_seq_lens, r, None, p.d_q, q)
+    assert (q == 7.0).all() and torch.equal(before.view(torch.int16), p.d_v_cache.view(torch.int16))
