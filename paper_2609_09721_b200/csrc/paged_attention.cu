@@ -101,19 +101,32 @@ __global__ void __launch_bounds__(128) paged_join_chunk_kernel(const __grid_cons
     float4 x[kGroups];
 #pragma unroll
     for (int u = 0; u < kGroups; ++u) x[u] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (int i = rec.first; i <= c; ++i) {
-        const int64_t at = (2 * i + (i == rec.first ? 1 : 0)) * 2 + half;
-        const float2 ml = __ldcg(A.part_ml + at * kChunkRows + r);
-        const float4* const part = reinterpret_cast<const float4*>(A.part_o + at * kChunkRows * kPagedD) + r;
-        float4 y[kGroups];
+    // two parts at a time: what a step costs is the wait for its loads
+    for (int i0 = rec.first; i0 <= c; i0 += 2) {
+        float2 ml[2];
+        float4 y[2][kGroups];
 #pragma unroll
-        for (int u = 0; u < kGroups; ++u) y[u] = __ldcg(part + (4 * u + warp) * kChunkRows);
-        const float upto = fmaxf(top, ml.x), base = upto == -INFINITY ? 0.0f : upto, before = paged_exp2(top - base), f = paged_exp2(ml.x - base);
+        for (int k = 0; k < 2; ++k) {
+            const int i = i0 + k;
+            ml[k] = make_float2(-INFINITY, 0.0f);
+#pragma unroll
+            for (int u = 0; u < kGroups; ++u) y[k][u] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (i <= c) {
+                const int64_t at = (2 * i + (i == rec.first ? 1 : 0)) * 2 + half;
+                ml[k] = __ldcg(A.part_ml + at * kChunkRows + r);
+                const float4* const part = reinterpret_cast<const float4*>(A.part_o + at * kChunkRows * kPagedD) + r;
+#pragma unroll
+                for (int u = 0; u < kGroups; ++u) y[k][u] = __ldcg(part + (4 * u + warp) * kChunkRows);
+            }
+        }
+        const float upto = fmaxf(top, fmaxf(ml[0].x, ml[1].x)), base = upto == -INFINITY ? 0.0f : upto, before = paged_exp2(top - base);
+        const float f0 = paged_exp2(ml[0].x - base), f1 = paged_exp2(ml[1].x - base);
         top = upto;
-        l = l * before + ml.y * f;
+        l = l * before + ml[0].y * f0 + ml[1].y * f1;
 #pragma unroll
         for (int u = 0; u < kGroups; ++u)
-            x[u] = make_float4(x[u].x * before + y[u].x * f, x[u].y * before + y[u].y * f, x[u].z * before + y[u].z * f, x[u].w * before + y[u].w * f);
+            x[u] = make_float4(x[u].x * before + y[0][u].x * f0 + y[1][u].x * f1, x[u].y * before + y[0][u].y * f0 + y[1][u].y * f1,
+                               x[u].z * before + y[0][u].z * f0 + y[1][u].z * f1, x[u].w * before + y[0][u].w * f0 + y[1][u].w * f1);
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
