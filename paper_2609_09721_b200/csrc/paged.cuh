@@ -33,6 +33,7 @@ template <> struct Pack2<__half> {
 };
 
 inline bool aligned_rows(const void* p, int64_t a, int64_t b, int64_t c) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ((a | b | c) & 7) == 0; }
+inline bool aligned_ints(const int32_t* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 // The cache's own fields; the tables' contents are looked at by the kernels.
 inline efq_status_t check_paged(const efq_paged_t& c, int d, int dtype)
@@ -42,6 +43,7 @@ inline efq_status_t check_paged(const efq_paged_t& c, int d, int dtype)
     if (dtype != EFQ_BF16 && dtype != EFQ_FP16) return EFQ_ERR_UNSUPPORTED;
     if (d != kPagedD || c.page_size < 16 || c.page_size > 4096 || (c.page_size & (c.page_size - 1)) != 0) return EFQ_ERR_UNSUPPORTED;
     if (static_cast<int64_t>(c.max_pages) * c.page_size >= (1ll << 31)) return EFQ_ERR_UNSUPPORTED;      // 32-bit indices of a sequence's tokens
+    if (!aligned_ints(c.page_table) || !aligned_ints(c.cu_seqlens) || !aligned_ints(c.seq_lens)) return EFQ_ERR_ALIGNMENT;
     if (c.k_page < 0 || c.k_head < 0 || c.k_token < 0 || c.v_page < 0 || c.v_head < 0 || c.v_token < 0) return EFQ_ERR_INVALID_ARG;
     if (!aligned_rows(c.k, c.k_page, c.k_head, c.k_token) || !aligned_rows(c.v, c.v_page, c.v_head, c.v_token)) return EFQ_ERR_ALIGNMENT;
     return EFQ_OK;

@@ -193,6 +193,10 @@ efq_status_t set_rows(RotaryRows& r, const efq_rows_t& g, bool with_dst, bool tu
 template <bool kPaged>
 efq_status_t launch(RotaryArgs& A, int dtype, bool interleaved, void* stream)
 {
+    if (!aligned_ints(A.positions)) return EFQ_ERR_ALIGNMENT;
+    const int64_t all_heads = static_cast<int64_t>(A.rows[0].heads) + A.rows[1].heads + A.rows[2].heads;
+    if (all_heads >= (1ll << 31) - 256) return EFQ_ERR_UNSUPPORTED;
+    A.heads = static_cast<int32_t>(all_heads);
     if (!device_is_sm100()) return EFQ_ERR_ARCH;
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return EFQ_ERR_CUDA;
@@ -236,7 +240,6 @@ extern "C" efq_status_t efq_rotary(const efq_rows_t* q, const efq_rows_t* k, con
     A.position_batch = position_batch;
     A.tokens = B * S;
     A.S = S;
-    A.heads = A.rows[0].heads + A.rows[1].heads;
     A.inverse = inverse ? 1 : 0;
     return efq::launch<false>(A, dtype, rotary->interleaved != 0, stream);
 }
@@ -267,7 +270,6 @@ extern "C" efq_status_t efq_paged_append(const efq_rows_t* k, const efq_rows_t* 
     A.positions = positions;
     A.position_axis = position_axis;
     A.tokens = A.S = total;
-    A.heads = A.rows[0].heads + A.rows[1].heads + A.rows[2].heads;
     A.page_table = cache->page_table;
     A.table_stride = cache->table_stride;
     A.cu_seqlens = cache->cu_seqlens;

@@ -202,3 +202,20 @@ def test_an_expired_wait_gives_rows_of_nan(n):
     torch.cuda.synchronize()
     assert torch.isnan(o).all()
     assert torch.equal(binding.efq_paged_attention_fwd(q, cache, cache, table, cu, lens, n, o=o, workspace=ws), want)
+
+
+def test_tables_and_positions_on_odd_addresses_are_refused():
+    """32-bit loads from an address that is no multiple of four fault."""
+    T = _rotation()
+    for name in ("page_table", "cu_seqlens", "seq_lens"):
+        bad = _cache(**{name: P + 2})
+        assert _attention(_rows(), bad) == ALIGNMENT and _append(_rows(heads=2), _rows(heads=2), cache=bad, rotation=T) == ALIGNMENT, name
+    assert _rotary(_rows(), positions=P + 2, rotation=T) == ALIGNMENT
+    R, K = _rows(heads=2), _cache()
+    assert binding.lib().efq_paged_append(C.byref(R), C.byref(R), None, 5, P + 1, 5, C.byref(K), 128, 0, C.byref(T), None) == ALIGNMENT
+
+
+def test_more_heads_than_32_bits_are_refused():
+    most = 2**31 - 1
+    assert _rotary(_rows(heads=most), _rows(heads=most), rotation=_rotation()) == UNSUPPORTED
+    assert _append(_rows(heads=2), _rows(heads=2), _rows(heads=most), cache=_cache()) == UNSUPPORTED
