@@ -185,6 +185,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
                         for (int i = 0; i < box * 16; ++i) reinterpret_cast<uint4*>(sm->kv[s] + row * 256)[i] = make_uint4(fill, fill, fill, fill);
                         ptx::fence_proxy_async_smem();
                     }
+                    __syncwarp();           // what the lanes have filled stands before lane 0's arrival
                     const uint32_t pages = __popc(__ballot_sync(0xffffffffu, page));
                     if (lane == 0) ptx::mbar_arrive_expect_tx(&sm->full[s], (A.inject_skip_loads ? 1u : pages) * static_cast<uint32_t>(box) * 256u);
                     __syncwarp();

@@ -97,6 +97,29 @@ def test_strides(lens, Hq, Hkv):
     assert torch.equal(odd[..., 8:], want[0]) and (odd[..., :8] == 7.0).all()
 
 
+@pytest.mark.parametrize("lens,Hq,Hkv", [([(1, 9000), (2, 77), (0, 3), (1, 1)], 8, 2), ([(200, 900), (3, 500), (130, 7000)], 8, 2), ([(33, 4000)], 3, 1)])
+def test_output_in_the_place_of_the_queries(lens, Hq, Hkv):
+    p = Paged(lens, Hq, Hkv, 32, seed=17)
+    want, _ = _run(p)
+    for _ in range(3):
+        q = p.d_q.clone()
+        binding.efq_paged_attention_fwd(q, p.d_k_cache, p.d_v_cache, *p.tables, p.max_q, o=q)
+        assert torch.equal(q, want)
+
+
+@pytest.mark.parametrize("n", [1, 100])
+def test_queries_and_pages_of_no_stride(n):
+    """One token's queries for all of them, one head's for all heads, and caches with a broadcast axis: dimensions with a stride of zero."""
+    p = Paged([(n, 700), (n, 90)], 8, 2, 16, seed=18)
+    for q in (p.d_q[:1].expand(p.total, -1, -1), p.d_q[:, :1].expand(-1, 8, -1), p.d_q[:1, :1].expand(p.total, 8, -1)):
+        want = binding.efq_paged_attention_fwd(q.contiguous(), p.d_k_cache, p.d_v_cache, *p.tables, p.max_q)
+        got = binding.efq_paged_attention_fwd(q, p.d_k_cache, p.d_v_cache, *p.tables, p.max_q, o=torch.empty_like(want))
+        assert torch.equal(got, want)
+    k = p.d_k_cache[:, :1].expand(-1, 2, -1, -1)
+    want = binding.efq_paged_attention_fwd(p.d_q, k.contiguous(), p.d_v_cache, *p.tables, p.max_q)
+    assert torch.equal(binding.efq_paged_attention_fwd(p.d_q, k, p.d_v_cache, *p.tables, p.max_q), want)
+
+
 @pytest.mark.parametrize("lens,Hq", [([(8, 3), (1, 0), (2, 500)], 2), ([(300, 100), (64, 0), (5, 5)], 2), ([(40, 1)], 32)])
 def test_tokens_that_see_nothing(lens, Hq):
     """More new tokens than tokens: the first ones see no key and get zeros, with lse = -inf."""
