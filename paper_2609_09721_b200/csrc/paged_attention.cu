@@ -198,15 +198,16 @@ efq_status_t encode_cache(CUtensorMap* map, int dtype, const void* base, int64_t
 }
 
 struct PagedPlan {
-    int rows;                            // of a part
+    int rows;                            // of a query tile
     size_t ml, records, total;
 };
 PagedPlan plan_paged(int64_t group_rows)
 {
     PagedPlan p;
-    p.rows = group_rows <= kFewRows ? kFewRows : 2 * kChunkRows;
-    p.ml = static_cast<size_t>(2 * kMaxCtas) * p.rows * kPagedD * 4;
-    p.records = p.ml + static_cast<size_t>(2 * kMaxCtas) * p.rows * sizeof(float2);
+    p.rows = group_rows <= kFewRows ? kFewRows : group_rows <= 2 * kFewRows ? 2 * kFewRows : 2 * kChunkRows;
+    const int room = p.rows > kFewRows ? 2 * kChunkRows : kFewRows;         // one size for all that is not a decode step
+    p.ml = static_cast<size_t>(2 * kMaxCtas) * room * kPagedD * 4;
+    p.records = p.ml + static_cast<size_t>(2 * kMaxCtas) * room * sizeof(float2);
     p.total = p.records + kMaxCtas * sizeof(PagedRecord);       // records on 16 bytes: 2 * kMaxCtas * rows is a multiple of 8
     return p;
 }
@@ -221,14 +222,14 @@ cudaError_t allow_smem(Kernel kernel, int bytes, std::atomic<uint64_t>& done, in
     return e;
 }
 
-template <typename T>
+template <typename T, int kRows>
 cudaError_t launch_few_rows(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const PagedArgs& A, int ctas, int max_rows, int dev, cudaStream_t st)
 {
     static std::atomic<uint64_t> done{0};
-    constexpr int smem = static_cast<int>(sizeof(FewSmem)) + 1024;
-    cudaError_t e = allow_smem(paged_few_kernel<T>, smem, done, dev);
-    if (e == cudaSuccess) e = launch_overlapped(paged_few_kernel<T>, dim3(static_cast<unsigned>(ctas)), kFewThreads, smem, st, mq, mk, mv, A);
-    if (e == cudaSuccess) e = launch_overlapped(paged_join_kernel<T, kFewRows>, dim3(static_cast<unsigned>(ctas), static_cast<unsigned>(max_rows)), 256, 0, st, A);
+    constexpr int smem = static_cast<int>(sizeof(FewSmem<kRows>)) + 1024;
+    cudaError_t e = allow_smem(paged_few_kernel<T, kRows>, smem, done, dev);
+    if (e == cudaSuccess) e = launch_overlapped(paged_few_kernel<T, kRows>, dim3(static_cast<unsigned>(ctas)), kFewThreads, smem, st, mq, mk, mv, A);
+    if (e == cudaSuccess) e = launch_overlapped(paged_join_kernel<T, kRows>, dim3(static_cast<unsigned>(ctas), static_cast<unsigned>(max_rows)), 256, 0, st, A);
     return e;
 }
 
@@ -260,7 +261,7 @@ efq_status_t paged_attention(const efq_rows_t* q, float* lse, int64_t total, int
     if (total == 0 || cache->n_seqs == 0) return EFQ_OK;
     const int64_t group_rows = static_cast<int64_t>(G) * (max_seqlen_q > 0 ? max_seqlen_q : 1);
     const PagedPlan plan = plan_paged(group_rows);
-    const bool many = plan.rows > kFewRows;
+    const bool many = plan.rows > 2 * kFewRows;
     const int step = many ? kChunkRows / G * 2 : plan.rows / G;         // new tokens of a query tile
     if (paged_most_units(total, cache->n_seqs, static_cast<int64_t>(cache->max_pages) * cache->page_size, cache->n_heads, step, many ? kChunkShift : kFewShift,
                          many ? kChunkItem : kFewItem) >= (1ll << 31))
@@ -312,8 +313,10 @@ efq_status_t paged_attention(const efq_rows_t* q, float* lse, int64_t total, int
     const int max_rows = group_rows < A.step * G ? static_cast<int>(group_rows) : A.step * G;       // the join's blocks; with more rows they go round
     using Bf = __nv_bfloat16;
     const bool bf = dtype == EFQ_BF16;
-    const cudaError_t e = many ? (bf ? launch_chunk<Bf>(mq, mk, mv, A, ctas, dev, s) : launch_chunk<__half>(mq, mk, mv, A, ctas, dev, s))
-                               : (bf ? launch_few_rows<Bf>(mq, mk, mv, A, ctas, max_rows, dev, s) : launch_few_rows<__half>(mq, mk, mv, A, ctas, max_rows, dev, s));
+    const auto few = plan.rows == kFewRows ? (bf ? launch_few_rows<Bf, kFewRows> : launch_few_rows<__half, kFewRows>)
+                                           : (bf ? launch_few_rows<Bf, 2 * kFewRows> : launch_few_rows<__half, 2 * kFewRows>);
+    const cudaError_t e = !many ? few(mq, mk, mv, A, ctas, max_rows, dev, s)
+                        : bf ? launch_chunk<Bf>(mq, mk, mv, A, ctas, dev, s) : launch_chunk<__half>(mq, mk, mv, A, ctas, dev, s);
     return e == cudaSuccess ? EFQ_OK : EFQ_ERR_CUDA;
 }
 

@@ -17,19 +17,21 @@ constexpr int kFewItem = 2;                     // what a query tile costs besid
 constexpr int kFewShift = 6, kFewKeys = 1 << kFewShift;       // of a stage
 constexpr int kFewWarps = 8;                    // that compute
 constexpr int kFewThreads = (kFewWarps + 1) * 32;
-constexpr int kFewRows = 16;
+constexpr int kFewRows = 16;                     // of a product; a query tile has 16 or 32 rows
 constexpr int kFewRowPad = 136;                 // floats of a row in the join: rows start 8 banks apart
 
+template <int kRows>
 struct __align__(1024) FewSmem {
     // Even, so that a stage's tiles all belong to one group of four warps: a group that skipped every other phase of a barrier could take the
     // phase before last for the last one, since loads may land in another order than they were issued in.
     static constexpr int kStages = 4;
     static_assert(kStages % 2 == 0, "a stage belongs to one group of warps");
+    static constexpr int kPeers = kFewWarps * kFewRows / kRows;         // warps that share a row's keys
     uint8_t k[kStages][kFewKeys * 256], v[kStages][kFewKeys * 256];     // [8 tokens][channels 0-63, 64-127][token], 128-byte swizzle
-    uint8_t q[2][2][kFewRows * 128];                                    // [channels 0-63, 64-127][row]
-    float join_o[kFewWarps / 2][kFewRows][kFewRowPad];
-    float2 join_ml[kFewWarps][kFewRows];
-    float2 row_ml[kFewRows];
+    uint8_t q[2][2][kRows * 128];                                       // [channels 0-63, 64-127][row]
+    float join_o[kPeers / 2][kRows][kFewRowPad];
+    float2 join_ml[kPeers][kRows];
+    float2 row_ml[kRows];
     uint64_t full[kStages], empty[kStages], q_full[2], q_empty[2];
     uint32_t scratch[kFewThreads / 32];
     PagedRun<kFewShift, kFewItem> run;
@@ -113,13 +115,14 @@ __device__ __forceinline__ void few_load_tile(Smem* sm, int stage, const CUtenso
                       max(entry, 0) * (is_v ? A.v_page_step : A.k_page_step) + g.head * (is_v ? A.v_head_step : A.k_head_step), &sm->full[stage]);
 }
 
-template <typename T>
+template <typename T, int kRows>
 __global__ void __launch_bounds__(kFewThreads, 1)
 paged_few_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
                  const __grid_constant__ PagedArgs A)
 {
-    using Smem = FewSmem;
-    constexpr int kStages = Smem::kStages;
+    static_assert(kRows == kFewRows || kRows == 2 * kFewRows, "the two groups of four warps");
+    using Smem = FewSmem<kRows>;
+    constexpr int kStages = Smem::kStages, kPeers = Smem::kPeers;
     extern __shared__ uint8_t smem_raw[];
     Smem* const sm = reinterpret_cast<Smem*>(smem_raw + ptx::smem_round_up(smem_raw, 1024u));
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -193,8 +196,11 @@ paged_few_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
     }
 
     // ---------------------------------------------------------------- scores, probabilities, output
-    const int sub = (warp & 3) * 16;                    // first of the warp's keys in a tile
+    // Of the four warps of a tile each has 16 rows, and 16 of the tile's keys, or 32 where there are 32 rows.
+    constexpr int kWide = kRows / kFewRows, kKeys = 16 * kWide, kSplit = 4 / kWide;
     const uint32_t group = warp >> 2;
+    const int sub = (warp % kSplit) * kKeys;            // first of the warp's keys in a tile
+    const int row0 = (warp & 3) / kSplit * 16, peer = static_cast<int>(group) * kSplit + warp % kSplit;      // its rows; its place among those that share them
     // the lane's row of a matrix of K (8 keys x 16 bytes) and of V; both have the swizzle of lane & 7
     const uint32_t k_at = ((sub >> 3) + (lane >> 4)) * 2048 + (lane & 7) * 128, v_at = ((sub >> 3) + ((lane >> 3) & 1)) * 2048 + (lane & 7) * 128;
     uint32_t tile = 0, seg = 0;
@@ -206,7 +212,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
         bool nan = !paged_wait_warp(&sm->q_full[qb], (seg >> 1) & 1u, sm) || g.w.none != 0;
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks) {
-            const uint32_t r = lane & 15, c = 2 * ks + (lane >> 4);
+            const uint32_t r = row0 + (lane & 15), c = 2 * ks + (lane >> 4);
             ldmatrix4(qa[ks], ptx::smem_u32(sm->q[qb][c >> 3]) + r * 128 + (((c & 7) ^ (r & 7)) << 4));
         }
         __syncwarp();
@@ -216,31 +222,42 @@ paged_few_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
 #pragma unroll
             for (int i = 0; i < 4; ++i) o[n][i] = 0.0f;
         ++seg;
-        const int limit[2] = {paged_limit(g, (lane >> 2) / A.G), paged_limit(g, (8 + (lane >> 2)) / A.G)};
+        const int limit[2] = {paged_limit(g, (row0 + (lane >> 2)) / A.G), paged_limit(g, (row0 + 8 + (lane >> 2)) / A.G)};
         const int fewest = paged_limit(g, 0);            // keys that every row sees
+        const bool idle = row0 >= g.tokens * A.G;        // no rows of the tile for this warp
 
         for (int j = g.j0; j < g.j1; ++j, ++tile) {
             if ((tile & 1u) != group) continue;
             const uint32_t stage = tile % kStages;
             if (!paged_wait_warp(&sm->full[stage], (tile / kStages) & 1u, sm)) { nan = true; continue; }
+            if (idle) {
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(&sm->empty[stage]);
+                continue;
+            }
             nan = nan || sm->bad[stage] != 0u;
             const int key0 = j * kFewKeys + sub;
-            float s[2][4];
+            float s[2 * kWide][4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s[0][i] = s[1][i] = 0.0f;
+            for (int n = 0; n < 2 * kWide; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[n][i] = 0.0f;
             const uint32_t kb = ptx::smem_u32(sm->k[stage]) + k_at;
 #pragma unroll
             for (int ks = 0; ks < 8; ++ks) {
                 const uint32_t c = 2 * ks + ((lane >> 3) & 1);
-                uint32_t b[4];
-                ldmatrix4(b, kb + (c >> 3) * 1024 + (((c & 7) ^ (lane & 7)) << 4));
-                mma16816<T>(s[0], qa[ks], b[0], b[1]);
-                mma16816<T>(s[1], qa[ks], b[2], b[3]);
+#pragma unroll
+                for (int h = 0; h < kWide; ++h) {
+                    uint32_t b[4];
+                    ldmatrix4(b, kb + h * 4096 + (c >> 3) * 1024 + (((c & 7) ^ (lane & 7)) << 4));
+                    mma16816<T>(s[2 * h], qa[ks], b[0], b[1]);
+                    mma16816<T>(s[2 * h + 1], qa[ks], b[2], b[3]);
+                }
             }
-            const bool whole = key0 + 16 <= fewest;
+            const bool whole = key0 + kKeys <= fewest;
             float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-            for (int n = 0; n < 2; ++n)
+            for (int n = 0; n < 2 * kWide; ++n)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     float x = s[n][i] * A.scale_log2;
@@ -272,72 +289,75 @@ paged_few_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
                 }
             }
 #pragma unroll
-            for (int n = 0; n < 2; ++n)
+            for (int n = 0; n < 2 * kWide; ++n)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     s[n][i] = paged_exp2(s[n][i] - base[i >> 1]);
                     l[i >> 1] += s[n][i];
                 }
-            // the scores' layout is that of the left operand: probabilities are rounded once, to the elements' type (half a step of
-            // 2^-8 or 2^-11 of each, its sum is kept unrounded)
-            const uint32_t p[4] = {Pack2<T>::round(s[0][0], s[0][1]), Pack2<T>::round(s[0][2], s[0][3]),
-                                   Pack2<T>::round(s[1][0], s[1][1]), Pack2<T>::round(s[1][2], s[1][3])};
-            // rows of V past the sequence hold whatever the page held, or what an earlier tile left: 0 times that has to be 0
-            const int valid = g.w.len - key0 - 2 * (lane & 3);
-            const uint32_t keep0 = valid >= 2 ? 0xffffffffu : valid == 1 ? 0xffffu : 0u, keep1 = valid >= 10 ? 0xffffffffu : valid == 9 ? 0xffffu : 0u;
-            const bool inside = key0 + 16 <= g.w.len;
             const uint32_t vb = ptx::smem_u32(sm->v[stage]) + v_at;
 #pragma unroll
-            for (int n = 0; n < 8; ++n) {
-                const uint32_t c = 2 * n + (lane >> 4);
-                uint32_t b[4];
-                ldmatrix4_trans(b, vb + (c >> 3) * 1024 + (((c & 7) ^ (lane & 7)) << 4));
-                if (!inside) {
-                    b[0] &= keep0; b[1] &= keep1; b[2] &= keep0; b[3] &= keep1;
+            for (int h = 0; h < kWide; ++h) {
+                // the scores' layout is that of the left operand: probabilities are rounded once, to the elements' type (half a step of
+                // 2^-8 or 2^-11 of each, its sum is kept unrounded)
+                const uint32_t p[4] = {Pack2<T>::round(s[2 * h][0], s[2 * h][1]), Pack2<T>::round(s[2 * h][2], s[2 * h][3]),
+                                       Pack2<T>::round(s[2 * h + 1][0], s[2 * h + 1][1]), Pack2<T>::round(s[2 * h + 1][2], s[2 * h + 1][3])};
+                // rows of V past the sequence hold whatever the page held, or what an earlier tile left: 0 times that has to be 0
+                const int key = key0 + 16 * h, valid = g.w.len - key - 2 * (lane & 3);
+                const uint32_t keep0 = valid >= 2 ? 0xffffffffu : valid == 1 ? 0xffffu : 0u, keep1 = valid >= 10 ? 0xffffffffu : valid == 9 ? 0xffffu : 0u;
+                const bool inside = key + 16 <= g.w.len;
+#pragma unroll
+                for (int n = 0; n < 8; ++n) {
+                    const uint32_t c = 2 * n + (lane >> 4);
+                    uint32_t b[4];
+                    ldmatrix4_trans(b, vb + h * 4096 + (c >> 3) * 1024 + (((c & 7) ^ (lane & 7)) << 4));
+                    if (!inside) {
+                        b[0] &= keep0; b[1] &= keep1; b[2] &= keep0; b[3] &= keep1;
+                    }
+                    mma16816<T>(o[2 * n], p, b[0], b[1]);
+                    mma16816<T>(o[2 * n + 1], p, b[2], b[3]);
                 }
-                mma16816<T>(o[2 * n], p, b[0], b[1]);
-                mma16816<T>(o[2 * n + 1], p, b[2], b[3]);
             }
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(&sm->empty[stage]);
         }
 
-        // -------------------------------------------------------- the eight warps' parts of the segment
+        // -------------------------------------------------------- the parts of the segment of the warps that share its rows
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             float& x = l[i];
             x += __shfl_xor_sync(0xffffffffu, x, 1);
             x += __shfl_xor_sync(0xffffffffu, x, 2);
             if (nan) x = __uint_as_float(0x7fc00000u);
-            if ((lane & 3) == 0) sm->join_ml[warp][8 * i + (lane >> 2)] = make_float2(m[i], x);
+            if ((lane & 3) == 0) sm->join_ml[peer][row0 + 8 * i + (lane >> 2)] = make_float2(m[i], x);
         }
         few_bar();
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const int r = 8 * i + (lane >> 2);
+            const int r = row0 + 8 * i + (lane >> 2);
             float top = -INFINITY, sum = 0.0f;
 #pragma unroll
-            for (int w = 0; w < kFewWarps; ++w) top = fmaxf(top, sm->join_ml[w][r].x);
+            for (int w = 0; w < kPeers; ++w) top = fmaxf(top, sm->join_ml[w][r].x);
             const float base = top == -INFINITY ? 0.0f : top;
 #pragma unroll
-            for (int w = 0; w < kFewWarps; ++w) sum += sm->join_ml[w][r].y * paged_exp2(sm->join_ml[w][r].x - base);
+            for (int w = 0; w < kPeers; ++w) sum += sm->join_ml[w][r].y * paged_exp2(sm->join_ml[w][r].x - base);
             const float f = paged_exp2(m[i] - base);
 #pragma unroll
             for (int n = 0; n < 16; ++n) {
                 o[n][2 * i] *= f;
                 o[n][2 * i + 1] *= f;
-                if (warp >= kFewWarps / 2)
-                    *reinterpret_cast<float2*>(&sm->join_o[warp - kFewWarps / 2][r][8 * n + 2 * (lane & 3)]) = make_float2(o[n][2 * i], o[n][2 * i + 1]);
+                if (peer >= kPeers / 2)
+                    *reinterpret_cast<float2*>(&sm->join_o[peer - kPeers / 2][r][8 * n + 2 * (lane & 3)]) = make_float2(o[n][2 * i], o[n][2 * i + 1]);
             }
-            if (warp == 0 && (lane & 3) == 0) sm->row_ml[r] = make_float2(top, sum);
+            if (peer == 0 && (lane & 3) == 0) sm->row_ml[r] = make_float2(top, sum);
         }
         few_bar();
-        if (warp < kFewWarps / 2) {
+        if (peer < kPeers / 2) {
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int n = 0; n < 16; ++n) {
-                    float2& x = *reinterpret_cast<float2*>(&sm->join_o[warp][8 * i + (lane >> 2)][8 * n + 2 * (lane & 3)]);
+                    float2& x = *reinterpret_cast<float2*>(&sm->join_o[peer][row0 + 8 * i + (lane >> 2)][8 * n + 2 * (lane & 3)]);
                     x = make_float2(x.x + o[n][2 * i], x.y + o[n][2 * i + 1]);
                 }
         }
@@ -348,7 +368,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
             const int r = i >> 5, c = 4 * (i & 31);
             float4 x = *reinterpret_cast<const float4*>(&sm->join_o[0][r][c]);
 #pragma unroll
-            for (int w = 1; w < kFewWarps / 2; ++w) {
+            for (int w = 1; w < kPeers / 2; ++w) {
                 const float4 y = *reinterpret_cast<const float4*>(&sm->join_o[w][r][c]);
                 x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
             }
@@ -360,8 +380,8 @@ paged_few_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
                     make_uint2(Pack2<T>::round(x.x * inv, x.y * inv), Pack2<T>::round(x.z * inv, x.w * inv));
                 if (A.lse != nullptr && c == 0) A.lse[static_cast<int64_t>(token) * (A.Hkv * A.G) + head] = ml.x * kLn2 + logf(ml.y);
             } else {
-                *reinterpret_cast<float4*>(A.part_o + (static_cast<int64_t>(slot) * kFewRows + r) * kPagedD + c) = x;
-                if (c == 0) A.part_ml[slot * kFewRows + r] = ml;
+                *reinterpret_cast<float4*>(A.part_o + (static_cast<int64_t>(slot) * kRows + r) * kPagedD + c) = x;
+                if (c == 0) A.part_ml[slot * kRows + r] = ml;
             }
         }
         if (tid == 0 && g.j0 > 0 && g.j1 == g.n)
