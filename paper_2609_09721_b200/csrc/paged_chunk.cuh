@@ -164,9 +164,18 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
             while (ok && walk.next(g)) {
                 const int end = max(chunk_half(g, 0, A.step).end, chunk_half(g, 1, A.step).end);
                 const int32_t* table = A.page_table + g.seq * A.table_stride;
+                // The tiles that every row sees may come in any order.  The CTAs of a head begin at other places of its keys; so that they read the
+                // same tiles at about the same time, tile t of a run is tile t of the sequence (round and round) wherever the segment has it.
+                const int body = max(0, min(end, paged_limit(g, 0) >> kChunkShift) - g.j0), around = max(g.w.len >> kChunkShift, 1);
+                const int want = static_cast<int>((slot >> 1) % static_cast<uint32_t>(around)), until = want <= g.j0 ? g.j0 - want : g.j0 + around - want;
+                const int shift = want >= g.j0 && want < g.j0 + body ? want - g.j0 : until < body ? body - until : 0;
+                auto place_of = [&](int j) {
+                    const int x = j + shift;
+                    return j >= g.j0 + body ? j : x >= g.j0 + body ? x - body : x;
+                };
                 // as it stands in the table: it is looked at when the tile after the next is loaded, so that nobody waits for it here
                 auto entry_of = [&](int j) {
-                    const int key = j * kChunkKeys + row, at = key >> A.page_shift;
+                    const int key = place_of(j) * kChunkKeys + row, at = key >> A.page_shift;
                     int e = -1;
                     if (row < kChunkKeys && j < end && key < g.w.len) e = __ldcg(table + at);
                     return e;
@@ -178,7 +187,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
                     const uint32_t s = slot % kChunkSlots;
                     if (slot >= kChunkSlots) ok = paged_wait_warp(&sm->empty[s], (slot / kChunkSlots - 1) & 1u, sm);
                     if (!ok) return;
-                    const int key = j * kChunkKeys + row;
+                    const int key = place_of(j) * kChunkKeys + row;
                     const bool mine = row < kChunkKeys && key < g.w.len, page = mine && entry >= 0 && !A.inject_skip_loads;
                     if (mine && entry < 0) {
 #pragma unroll 1
