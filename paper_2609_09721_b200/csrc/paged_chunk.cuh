@@ -24,10 +24,24 @@ constexpr int kChunkPart = kChunkKeys * 128;                   // bytes of 64 ch
 constexpr uint32_t kChunkColS = 0, kChunkColO = 256;           // + 128 for the second half
 constexpr float kSlack = 8.0f;                                 // log2: probabilities stay below 2^8, sums below 2^8 times the keys
 
+// A segment of the run, as the warps that load tell it to the others: found out once, since the code of the walk is run rarely and not at hand when it is
+// (each of the others walking for itself: 3300 clocks between two segments).  Of [2] one for each half.
+struct __align__(16) ChunkSegment {
+    int32_t j0;                                                // first key tile; -1: the run has ended
+    int32_t end[2];                                            // key tiles [j0, end) are seen by the half
+    int32_t fewest[2];                                         // keys that every row of the half sees
+    int32_t tokens[2];
+    int32_t token0, head, len, base;                           // as in PagedSegment
+    int32_t none, all, record;                                 // rows of NaN; the whole query tile; its end, begun by another CTA
+};
+constexpr int kChunkSegments = 4;
+
 struct __align__(1024) ChunkSmem {
     uint8_t q[2][2][kChunkPart];                               // half, channels 0-63 and 64-127; 128-byte swizzle
     uint8_t kv[kChunkSlots][2 * kChunkPart];                   // [8 tokens][channels 0-63, 64-127][token]
     uint64_t full[kChunkSlots], empty[kChunkSlots], q_full, q_empty, s_full[2], p_ready[2], p_rest[2], o_full[2], v_tail, v_clean, drained[2];
+    uint64_t seg_full[kChunkSegments], seg_empty[kChunkSegments];
+    ChunkSegment seg[kChunkSegments];
     uint32_t scratch[kChunkThreads / 32];
     PagedRun<kChunkShift, kChunkItem> run;
     uint32_t tmem_base;
@@ -100,18 +114,35 @@ __device__ __forceinline__ void store8(void* p, const uint32_t (&u)[8])
 template <typename V>
 __device__ __forceinline__ V uniform(V x) { return __shfl_sync(0xffffffffu, x, 0); }
 
-// Of a segment: tokens of a half, and the key tiles of the run that it needs: [j0, end).
-struct ChunkHalf {
-    int tokens, end;
-};
-__device__ __forceinline__ ChunkHalf chunk_half(const PagedSegment<kChunkShift, kChunkItem>& g, int half, int step)
+__device__ __forceinline__ ChunkSegment chunk_segment(const PagedSegment<kChunkShift, kChunkItem>& g, int step)
 {
     const int per = step >> 1;
-    ChunkHalf h;
-    h.tokens = max(0, min(per, g.tokens - half * per));
-    const int seen = h.tokens > 0 ? paged_limit(g, half * per + h.tokens - 1) : 0;
-    h.end = max(g.j0, min(g.j1, (seen + kChunkKeys - 1) >> kChunkShift));
-    return h;
+    ChunkSegment d;
+    d.j0 = g.j0;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        d.tokens[w] = max(0, min(per, g.tokens - w * per));
+        const int seen = d.tokens[w] > 0 ? paged_limit(g, w * per + d.tokens[w] - 1) : 0;
+        d.end[w] = max(g.j0, min(g.j1, (seen + kChunkKeys - 1) >> kChunkShift));
+        d.fewest[w] = d.tokens[w] > 0 ? paged_limit(g, w * per) : 0;
+    }
+    d.token0 = g.token0;
+    d.head = g.head;
+    d.len = g.w.len;
+    d.base = g.base;
+    d.none = g.w.none;
+    d.all = g.j0 == 0 && g.j1 == g.n ? 1 : 0;
+    d.record = g.j0 > 0 && g.j1 == g.n ? 1 : 0;
+    return d;
+}
+// The wait for a segment, or for the room of one.  It goes on when another wait has expired, since the rows of the segments that are left become
+// NaN then: their warps let go of them without one, so two seconds are more than any of these waits can take.
+__device__ __forceinline__ bool chunk_segment_wait(uint64_t* bar, uint32_t parity)
+{
+    bool there = ptx::mbar_try_wait(bar, parity);
+#pragma unroll 1
+    for (int i = 0; !there && i < 40000; ++i) there = ptx::mbar_try_wait_suspend(bar, parity, 50000u);
+    return __all_sync(0xffffffffu, there) != 0;
 }
 
 template <typename T>
@@ -132,6 +163,10 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
         ptx::mbar_init(&sm->q_empty, 2);
         ptx::mbar_init(&sm->v_tail, 1);
         ptx::mbar_init(&sm->v_clean, 1);
+        for (int i = 0; i < kChunkSegments; ++i) {
+            ptx::mbar_init(&sm->seg_full[i], 1);
+            ptx::mbar_init(&sm->seg_empty[i], 11);             // the warps but the one that loads
+        }
         for (int i = 0; i < 2; ++i) {
             ptx::mbar_init(&sm->s_full[i], 1);
             ptx::mbar_init(&sm->p_ready[i], 5);
@@ -151,18 +186,41 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
     paged_find_run<kChunkThreads, kChunkShift, kChunkItem>(A, sm->scratch, &sm->run);      // barriers of the block
     ptx::tc_fence_after_sync();
     const uint32_t tmem = sm->tmem_base;
-    PagedWalk<kChunkShift, kChunkItem, PagedReader<kChunkShift, kChunkItem>> walk(PagedReader<kChunkShift, kChunkItem>{A}, A.n_seqs, A.Hkv, sm->run);
-    PagedSegment<kChunkShift, kChunkItem> g;
+    uint32_t seg = 0;           // segments so far
+    // the next one; false at the end of the run
+    auto next = [&](ChunkSegment& d) {
+        const uint32_t at = seg % kChunkSegments;
+        if (!chunk_segment_wait(&sm->seg_full[at], (seg / kChunkSegments) & 1u)) return false;
+        d = sm->seg[at];
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(&sm->seg_empty[at]);
+        ++seg;
+        return d.j0 >= 0;
+    };
+    ChunkSegment d;
 
     if (warp >= 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kChunkRegsLess));
         if (warp == 9) {
             // ------------------------------------------------------------ loads
             const int P = 1 << A.page_shift, box = min(P, kChunkKeys), row = lane * box;
+            PagedWalk<kChunkShift, kChunkItem, PagedReader<kChunkShift, kChunkItem>> walk(PagedReader<kChunkShift, kChunkItem>{A}, A.n_seqs, A.Hkv, sm->run);
+            PagedSegment<kChunkShift, kChunkItem> g;
             uint32_t slot = 0, q_loads = 0;          // loads so far
             bool ok = true;
-            while (ok && walk.next(g)) {
-                const int end = max(chunk_half(g, 0, A.step).end, chunk_half(g, 1, A.step).end);
+            for (bool more = true; more; ++seg) {
+                more = walk.next(g);
+                if (more) d = chunk_segment(g, A.step);
+                else d.j0 = -1;
+                const uint32_t at = seg % kChunkSegments;
+                if (seg >= kChunkSegments && !chunk_segment_wait(&sm->seg_empty[at], (seg / kChunkSegments - 1) & 1u)) break;
+                if (lane == 0) {
+                    sm->seg[at] = d;
+                    ptx::mbar_arrive(&sm->seg_full[at]);
+                }
+                __syncwarp();
+                if (!more || !ok) continue;          // after a wait that has expired the segments are told all the same
+                const int end = max(d.end[0], d.end[1]);
                 const int32_t* table = A.page_table + g.seq * A.table_stride;
                 // The tiles that every row sees may come in any order.  The CTAs of a head begin at other places of its keys; so that they read the
                 // same tiles at about the same time, tile t of a run is tile t of the sequence (round and round) wherever the segment has it.
@@ -201,13 +259,13 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
                     if (page) tma_load_page(sm->kv[s] + row * 256, &map, (key & (P - 1)) >> 3, entry * page_step + g.head * head_step, &sm->full[s]);
                     ++slot;
                 };
-                int entry = entry_of(g.j0), next = entry_of(g.j0 + 1);
+                int entry = entry_of(g.j0), entry_next = entry_of(g.j0 + 1);
                 for (int j = g.j0; ok && j < end; ++j) {
                     const int ahead = entry_of(j + 2);
                     load(mk, A.k_page_step, A.k_head_step, j, entry, 0x7fff7fffu);
                     if (ok && j == g.j0) {
                         if (q_loads > 0) ok = paged_wait_warp(&sm->q_empty, (q_loads - 1) & 1u, sm);
-                        if (!ok) break;
+                        if (!ok) break;             // of this segment's loads
                         if (ptx::elect_one()) {
                             const int per = A.step >> 1;
                             ptx::mbar_arrive_expect_tx(&sm->q_full, static_cast<uint32_t>(A.step * A.G) * 256u);
@@ -218,8 +276,8 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
                         ++q_loads;
                     }
                     if (ok) load(mv, A.v_page_step, A.v_head_step, j, entry, 0u);
-                    entry = next;
-                    next = ahead;
+                    entry = entry_next;
+                    entry_next = ahead;
                 }
             }
             if (lane == 0) {        // its copies in flight end before the block does, whatever the others do
@@ -271,16 +329,16 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
                 ptx::mma_commit(s_full);
                 ptx::mma_commit(&sm->empty[slot]);
             };
-            while (ok && walk.next(g)) {
-                const int e0 = chunk_half(g, 0, A.step).end, e1 = chunk_half(g, 1, A.step).end;
-                const int j0 = uniform(g.j0), mine = uniform(w ? e1 : e0), other = uniform(w ? e0 : e1), end = uniform(max(e0, e1)), clean = uniform(g.w.len < max(e0, e1) * kChunkKeys ? 1 : 0);
-                if (end == j0) continue;
+            while (next(d)) {
+                const int j0 = uniform(d.j0), mine = uniform(w ? d.end[1] : d.end[0]), other = uniform(w ? d.end[0] : d.end[1]), end = max(mine, other);
+                const int clean = uniform(d.len < end * kChunkKeys ? 1 : 0);
+                if (!ok || end == j0) continue;
                 ok = paged_wait_warp(&sm->q_full, q_round, sm) && paged_wait_warp(&sm->full[slot], round, sm);
                 q_round ^= 1u;
                 // the first scores; half 1 gives half 0 the turn for the first tile
                 const bool opens = w == 1 && j0 < other;
                 if (opens) ok = ok && turn_taken();
-                if (!ok) break;
+                if (!ok) continue;
                 if (ptx::elect_one()) {
                     if (j0 < mine) {
                         scores(opens);
@@ -360,13 +418,13 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
             // They hold whatever the page held, and 0 times that has to be 0.
             uint32_t slot = 0, round = 0;           // loads so far; parity of the next wait
             bool ok = true;
-            while (ok && walk.next(g)) {
-                const int end = max(chunk_half(g, 0, A.step).end, chunk_half(g, 1, A.step).end), inside = g.w.len - (end - 1) * kChunkKeys;
-                if (end == g.j0) continue;
-                slot += 2 * (end - g.j0);
-                if (inside >= kChunkKeys) continue;
+            while (next(d)) {
+                const int end = max(d.end[0], d.end[1]), inside = d.len - (end - 1) * kChunkKeys;
+                if (end == d.j0) continue;
+                slot += 2 * (end - d.j0);
+                if (!ok || inside >= kChunkKeys) continue;
                 ok = paged_wait_warp(&sm->v_tail, round, sm);
-                if (!ok) break;
+                if (!ok) continue;
                 round ^= 1u;
                 uint8_t* const v = sm->kv[(slot - 1) % kChunkSlots];
 #pragma unroll 1
@@ -388,14 +446,14 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
         const int i = w * per + r / A.G;         // token of the tile
         uint32_t s_count = 0, o_count = 0;
         if (tid == 0) A.records[blockIdx.x].first = -1;
-        while (walk.next(g)) {
-            const ChunkHalf h = chunk_half(g, w, A.step);
-            const bool mine = r < h.tokens * A.G;
-            const int limit = paged_limit(g, i);
-            const int fewest = h.tokens > 0 ? paged_limit(g, w * per) : 0;      // keys that every row of the half sees
-            bool nan = g.w.none != 0;
+        while (next(d)) {
+            // what decides the loop's course is the same in all lanes (2048 tokens on 32768 930 us without the compiler knowing it, 904 with)
+            const int j0 = uniform(d.j0), end = uniform(w ? d.end[1] : d.end[0]), fewest = uniform(w ? d.fewest[1] : d.fewest[0]);
+            const bool mine = r < uniform((w ? d.tokens[1] : d.tokens[0]) * A.G);
+            const int limit = A.causal ? max(0, min(d.len, d.base + i + 1)) : d.len;
+            bool nan = d.none != 0;
             float m = -INFINITY, l = 0.0f;
-            for (int j = g.j0; j < h.end; ++j) {
+            for (int j = j0; j < end; ++j) {
                 if (!paged_wait_warp(&sm->s_full[w], s_count & 1u, sm)) { nan = true; break; }
                 ++s_count;
                 ptx::tc_fence_after_sync();
@@ -425,7 +483,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
                     const float alpha = grew ? (m == -INFINITY ? 0.0f : paged_exp2(m - mx)) : 1.0f;
                     if (grew) m = mx < INFINITY ? mx : __uint_as_float(0x7fc00000u);      // an infinite score makes a row of NaN, as inf - inf does
                     l *= alpha;
-                    if (j > g.j0) {
+                    if (j > j0) {
 #pragma unroll 1
                         for (int q = 0; q < 4; ++q) {
                             float o[32];
@@ -468,14 +526,14 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
                 l += sum2[0].x + sum2[0].y;
             }
 
-            const bool some = h.end > g.j0, all = g.j0 == 0 && g.j1 == g.n;
+            const bool some = end > j0, all = d.all != 0;
             if (some && !nan) {
                 nan = !paged_wait_warp(&sm->o_full[w], o_count & 1u, sm);
                 ++o_count;
                 ptx::tc_fence_after_sync();
             }
             if (nan) l = __uint_as_float(0x7fc00000u);
-            const int token = g.token0 + i, head = g.head * A.G + r % A.G, slot = 2 * blockIdx.x + (g.j0 == 0 ? 1 : 0);
+            const int token = d.token0 + i, head = d.head * A.G + r % A.G, slot = 2 * blockIdx.x + (j0 == 0 ? 1 : 0);
             const float inv = l == 0.0f ? 0.0f : 1.0f / l;
             char* const dst = A.o + token * A.o_token + head * A.o_head;
             // of four channels the 128 rows side by side, so that a warp's stores are whole lines
@@ -512,7 +570,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
             ptx::tc_fence_before_sync();
             if (mine && all && A.lse != nullptr) A.lse[static_cast<int64_t>(token) * (A.Hkv * A.G) + head] = m * kLn2 + logf(l);
             if (mine && !all) A.part_ml[slot * 2 * kChunkRows + w * kChunkRows + r] = make_float2(m, l);
-            if (tid == 0 && g.j0 > 0 && g.j1 == g.n) A.records[blockIdx.x] = {sm->run.begins, g.token0, g.tokens, g.head};
+            if (tid == 0 && d.record) A.records[blockIdx.x] = {sm->run.begins, d.token0, d.tokens[0] + d.tokens[1], d.head};
         }
     }
     ptx::tc_fence_before_sync();
