@@ -5,7 +5,7 @@
 // for the softmax of each half, one for each half that issues its MMAs, one that loads, one that clears rows of V past a sequence.  While the softmax warps of one half are busy, the tensor core
 // has the other half's products: per half and tile Q K^T (both operands in shared memory), then P V (P from tensor memory).
 //   - A thread has a row, so maxima and sums need no other thread.  The output is rescaled in tensor memory by the same threads,
-//     only when a row's maximum has grown by more than 2^8 (kSlack); the sum refers to the same maximum, so the result is exact.  When
+//     only when a row's maximum has grown by more than 2^14 (kSlack); the sum refers to the same maximum, so the result is exact.  When
 //     the scores of a tile are there, the product of the tile before has ended (the tensor core works in order), so nobody waits for it.
 //   - K and V come through one ring of 32 KB slots, pages by TMA; 64 KB hold Q.
 // Bound by the exponentials and the MMAs, which take the same time: a tile of 256 x 128 scores is 32768 exponentials at 16 a clock and
@@ -22,7 +22,9 @@ constexpr int kChunkThreads = 384;
 constexpr int kChunkSlots = 5;
 constexpr int kChunkPart = kChunkKeys * 128;                   // bytes of 64 channels of 128 rows
 constexpr uint32_t kChunkColS = 0, kChunkColO = 256;           // + 128 for the second half
-constexpr float kSlack = 8.0f;                                 // log2: probabilities stay below 2^8, sums below 2^8 times the keys
+// log2: probabilities stay below 2^14 (fp16 ends at 2^16), sums below 2^14 times the keys.  Scores that spread as under outlier channels: 2048 tokens on
+// 32768 884 us with 8, 874 with 14, a mixed batch 274 and 271.
+constexpr float kSlack = 14.0f;
 
 // A segment of the run, as the warps that load tell it to the others: found out once, since the code of the walk is run rarely and not at hand when it is
 // (each of the others walking for itself: 3300 clocks between two segments).  Of [2] one for each half.
@@ -80,7 +82,7 @@ __device__ __forceinline__ float max3(float a, float b, float c)
     asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
 }
-// 2^x for x <= 8 on the FMA pipe: x = n + f with n the nearest integer, 1 + f q(f) with q of degree 3 fitted to the smallest relative error on
+// 2^x for x <= 14 on the FMA pipe: x = n + f with n the nearest integer, 1 + f q(f) with q of degree 3 fitted to the smallest relative error on
 // [-1/2, 1/2] (least squares, reweighted until the error is level: 2.9e-6, a thousandth of what rounding the probability costs), n added
 // to the exponent.  Below -127 the result is 0, exactly: f = 0 there and the exponent field is empty.  NaN is not kept.
 __device__ __forceinline__ float2 poly_exp2(float2 x)
