@@ -197,6 +197,10 @@ efq_status_t encode_cache(CUtensorMap* map, int dtype, const void* base, int64_t
     return encode(map, dtype, base, 5, dims, strides, box) ? EFQ_OK : EFQ_ERR_CUDA;
 }
 
+// Which kernel: by the rows that the query heads of a KV group and the announced tokens make.  Up to 16, and up to 32: the kernel for few rows with one or
+// two groups of them, else that for many.  The lines, both sides measured (32 / 8 heads, us): 16 rows by two groups 16 sequences of 4 tokens on 5000 keys
+// 63.9 and 67.0, one of 4 on 8000 14.6 and 14.8, 60 of 4 on 700 43.7 and 46.3, 64 of 1 on 5000 223 and 229; 32 rows by the kernel for many 16 of 8 on
+// 5000 74.2 and 74.5, one of 8 on 8000 17.5 and 22.9, 60 of 8 on 700 53.5 and 49.9, 60 of 5 on 700 48.7 and 50.4.
 struct PagedPlan {
     int rows;                            // of a query tile
     size_t ml, records, total;

@@ -2,21 +2,28 @@
 //
 // A query tile is two halves of up to 128 rows (tokens of the chunk times the query heads of the KV group, whole tokens only), each with
 // its scores (128 columns of tensor memory, whose first 64 take the probabilities afterwards) and its output (128 columns).  Twelve warps: four
-// for the softmax of each half, one for each half that issues its MMAs, one that loads, one that clears rows of V past a sequence.  While the softmax warps of one half are busy, the tensor core
-// has the other half's products: per half and tile Q K^T (both operands in shared memory), then P V (P from tensor memory).
+// for the softmax of each half, one for each half that issues its MMAs, one that loads and tells the others what comes next, one that clears rows
+// of V past a sequence.  While the softmax warps of one half are busy, the tensor core has the other half's products: per half and tile Q K^T (both
+// operands in shared memory), then P V (P from tensor memory).
 //   - A thread has a row, so maxima and sums need no other thread.  The output is rescaled in tensor memory by the same threads,
 //     only when a row's maximum has grown by more than 2^14 (kSlack); the sum refers to the same maximum, so the result is exact.  When
 //     the scores of a tile are there, the product of the tile before has ended (the tensor core works in order), so nobody waits for it.
 //   - K and V come through one ring of 32 KB slots, pages by TMA; 64 KB hold Q.
-// Bound by the exponentials and the MMAs, which take the same time: a tile of 256 x 128 scores is 32768 exponentials at 16 a clock and
-// 4 x 128 x 128 x 128 products at 4096 a clock, 2048 clocks each.
+//   - The CTAs of a head read the same tiles at about the same time, so that L2 has them once and not every CTA's own part of a long context.
+// 2048 tokens on 32768 keys (32 / 8 heads): 890 us, 1.20 PFLOP/s of the 1.65 of the library's product.  A tile of 256 x 128 scores takes 2064 clocks of the
+// tensor core and some 2950 in all: a half's scores (512), softmax (1700, of which 768 exponentials at 16 a clock an SM) and what is left of its products
+// follow one another, and there is no room in tensor memory for its next scores meanwhile.  Calls in a row run at the board's power limit, 1.46 GHz
+// instead of 1.97 (one alone takes 780 us), so what saves instructions and traffic counts as much as what shortens the chain.  Between two
+// query tiles some 5000 clocks are lost.
 #pragma once
 
 #include "paged_few.cuh"
 
 namespace efq {
 
-constexpr int kChunkItem = 2;                                  // what a query tile costs beside its key tiles, in key tiles
+// What a query tile costs beside its key tiles, in key tiles.  With 0, 1, 2 and 3: a mixed batch of 16 sequences 290, 281, 276 and 279 us, 300 tokens on
+// 9000 59.6, 58.1, 57.0 and 57.2, 64 on 2000 21.5, 21.4, 21.5 and 22.2.
+constexpr int kChunkItem = 2;
 constexpr int kChunkShift = 7, kChunkKeys = 1 << kChunkShift, kChunkRows = 128;      // keys of a tile, rows of a half
 constexpr int kChunkThreads = 384;
 constexpr int kChunkSlots = 5;
@@ -50,7 +57,8 @@ struct __align__(1024) ChunkSmem {
     volatile uint32_t failed;
 };
 
-// Registers of a softmax thread, which holds a row of scores, and of the others: together what the block is launched with, 384 x 168.
+// Registers of a softmax thread, which holds a row of scores, and of the others: together what the block is launched with, 384 x 168.  208 and 88: 2048
+// tokens on 32768 943 us and 889, 224 and 56: 942 and 904.
 constexpr int kChunkRegsMore = 216, kChunkRegsLess = 72;
 static_assert(256 * kChunkRegsMore + 128 * kChunkRegsLess <= 384 * 168, "setmaxnreg draws on what the block was launched with");
 
@@ -523,6 +531,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
                             if (lane == 0) ptx::mbar_arrive(&sm->p_ready[w]);
                         }
                         float2 y = fma2(make_float2(s[32 * q + 2 * c], s[32 * q + 2 * c + 1]), scale2, minus2);
+                        // a quarter of the exponentials by polynomial (an eighth: 946 us and 889, three eighths: 903)
                         y = c % 4 == 3 ? poly_exp2(y) : make_float2(paged_exp2(y.x), paged_exp2(y.y));
                         sum2[c & 1] = add2(sum2[c & 1], y);
                         // rounded once, to the elements' type (half a step of 2^-8 or 2^-11 of each); the sum is kept unrounded
