@@ -11,7 +11,7 @@
 //   - K and V come through one ring of 32 KB slots, pages by TMA; 64 KB hold Q.
 //   - The CTAs of a head read the same tiles at about the same time, so that L2 has them once and not every CTA's own part of a long context.
 // 2048 tokens on 32768 keys (32 / 8 heads): 890 us, 1.20 PFLOP/s of the 1.65 of the library's product.  A tile of 256 x 128 scores takes 2064 clocks of the
-// tensor core and some 2950 in all: a half's scores (512), softmax (1700, of which 768 exponentials at 16 a clock an SM) and what is left of its products
+// tensor core and some 2800 in all: a half's scores (512), softmax (1600, of which 768 exponentials at 16 a clock an SM) and what is left of its products
 // follow one another, and there is no room in tensor memory for its next scores meanwhile.  Calls in a row run at the board's power limit, 1.46 GHz
 // instead of 1.97 (one alone takes 780 us), so what saves instructions and traffic counts as much as what shortens the chain.  Between two
 // query tiles some 5000 clocks are lost.
@@ -553,6 +553,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
                 ++o_count;
                 ptx::tc_fence_after_sync();
             }
+            nan = nan || sm->failed != 0u;          // once a wait has expired the parities of the later ones mean nothing
             if (nan) l = __uint_as_float(0x7fc00000u);
             const int token = d.token0 + i, head = d.head * A.G + r % A.G, slot = 2 * blockIdx.x + (j0 == 0 ? 1 : 0);
             const float inv = l == 0.0f ? 0.0f : 1.0f / l;

@@ -326,6 +326,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
         }
 
         // -------------------------------------------------------- the parts of the segment of the warps that share its rows
+        nan = nan || sm->failed != 0u;          // once a wait has expired the parities of the later ones mean nothing
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             float& x = l[i];

@@ -204,6 +204,27 @@ def test_an_expired_wait_gives_rows_of_nan(n):
     assert torch.equal(binding.efq_paged_attention_fwd(q, cache, cache, table, cu, lens, n, o=o, workspace=ws), want)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [1, 6, 20])
+def test_an_expired_wait_in_a_step_of_many_sequences(n):
+    """Blocks have many query tiles to go when the first wait runs out: all their rows become NaN, those without a key are zeros as ever."""
+    seqs = 400
+    g = torch.Generator(device="cuda").manual_seed(2)
+    q = torch.randn(seqs * n, 8, 128, generator=g, device="cuda").bfloat16()
+    cache = torch.randn(64, 2, 16, 128, generator=g, device="cuda").bfloat16()
+    table = torch.randint(0, 64, (seqs, 12), generator=g, dtype=torch.int32, device="cuda")
+    cu = torch.arange(0, seqs * n + 1, n, dtype=torch.int32, device="cuda")
+    lens = torch.tensor([0 if i % 7 == 3 else n + (i * 11) % 170 for i in range(seqs)], dtype=torch.int32, device="cuda")
+    want = binding.efq_paged_attention_fwd(q, cache, cache, table, cu, lens, n)
+    o = torch.zeros_like(q)
+    ws = torch.empty(binding.efq_paged_attention_workspace_bytes(8, 2, n), dtype=torch.uint8, device="cuda")
+    binding.efq_paged_attention_fwd_inject_timeout(q, cache, cache, table, cu, lens, n, o, ws)
+    torch.cuda.synchronize()
+    seen = (lens > 0).repeat_interleave(n)
+    assert torch.isnan(o[seen]).all() and (torch.isnan(o[~seen]) | (o[~seen] == 0)).all()
+    assert torch.equal(binding.efq_paged_attention_fwd(q, cache, cache, table, cu, lens, n, o=o, workspace=ws), want)
+
+
 def test_tables_and_positions_on_odd_addresses_are_refused():
     """32-bit loads from an address that is no multiple of four fault."""
     T = _rotation()
