@@ -97,6 +97,31 @@ def test_strides(lens, Hq, Hkv):
     assert torch.equal(odd[..., 8:], want[0]) and (odd[..., :8] == 7.0).all()
 
 
+# rows of a KV group from 17 to 32 in the longest sequence, fewer in others: warps without rows, sequences without tokens or keys
+MIDDLE = [
+    ([(5, 300), (1, 200), (2, 64), (0, 5), (5, 5), (3, 1), (4, 1000), (1, 1)], 8, 2, 16), ([(8, 70), (1, 5000), (8, 4097), (5, 63)], 8, 2, 64),
+    ([(1, 100 + 61 * i) for i in range(90)], 32, 1, 32), ([(1 + i % 5, 6 + 40 * i) for i in range(70)], 20, 4, 16), ([(2, 3000), (1, 2999)], 32, 2, 128),
+    ([(1, 1), (1, 64), (1, 65)], 17, 1, 16), ([(32, 32), (31, 700), (1, 700), (16, 40), (17, 40)], 3, 3, 16),
+]
+
+
+@pytest.mark.parametrize("lens,Hq,Hkv,page", MIDDLE)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_17_to_32_rows(lens, Hq, Hkv, page, dtype):
+    p = Paged(lens, Hq, Hkv, page, seed=19, dtype=dtype, tail=3)
+    _check(p, *_run(p))
+    o, _ = _run(p, causal=False)
+    _check(p, o, None, causal=False)
+
+
+@pytest.mark.parametrize("lens,Hq,Hkv", [([(150, 20000)], 2, 1), ([(40, 9000), (300, 12345), (1, 7000)], 4, 2), ([(64, 30000)], 8, 4)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_runs_that_begin_inside_long_contexts(lens, Hq, Hkv, causal):
+    """The tiles of such a run are read in another order than that of the keys."""
+    p = Paged(lens, Hq, Hkv, 128, seed=20)
+    _check(p, *_run(p, causal), causal=causal)
+
+
 @pytest.mark.parametrize("lens,Hq,Hkv", [([(1, 9000), (2, 77), (0, 3), (1, 1)], 8, 2), ([(200, 900), (3, 500), (130, 7000)], 8, 2), ([(33, 4000)], 3, 1)])
 def test_output_in_the_place_of_the_queries(lens, Hq, Hkv):
     p = Paged(lens, Hq, Hkv, 32, seed=17)
