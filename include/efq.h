@@ -380,8 +380,8 @@ efq_status_t efq_paged_append(const efq_rows_t* k, const efq_rows_t* v, const ef
  * Scores, maxima, sums and the output's accumulator are FP32, the probabilities of a tile are rounded to the elements' type for the product
  * with V.  A token that sees no key gets a row of zeros and lse = -inf.  Rows behind cu_seqlens[n_seqs] are left alone.  What lies in the pages
  * behind a sequence's last token does not matter; an infinity or NaN in a value of the sequence makes NaN of its channel in
- * every row of the 128 x 128 tiles that hold it.  Rows are NaN where the page table names no page (an entry below
- * zero or from n_pages on, a sequence longer than max_pages * page_size), and in blocks in which a bounded device-side wait expired.
+ * every row of the 128 x 128 tiles that hold it.  Rows are NaN that see a key for which the page table names no page (an entry below
+ * zero or from n_pages on), those of a sequence longer than max_pages * page_size, and in blocks in which a bounded device-side wait expired.
  * Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, WORKSPACE, ARCH, CUDA.  total == 0 or n_seqs == 0 is a valid no-op. */
 size_t efq_paged_attention_workspace_bytes(int Hq, int Hkv, int max_seqlen_q, int d);
 efq_status_t efq_paged_attention_fwd(const efq_rows_t* q, float* lse, int64_t total, int max_seqlen_q, const efq_paged_t* cache, int d,

@@ -22,6 +22,7 @@ constexpr int kFewWarps = 8;                    // that compute
 constexpr int kFewThreads = (kFewWarps + 1) * 32;
 constexpr int kFewRows = 16;                     // of a product; a query tile has 16 or 32 rows
 constexpr int kFewRowPad = 136;                 // floats of a row in the join: rows start 8 banks apart
+constexpr int kNoKey = 0x7fffffff;
 
 template <int kRows>
 struct __align__(1024) FewSmem {
@@ -38,7 +39,7 @@ struct __align__(1024) FewSmem {
     uint64_t full[kStages], empty[kStages], q_full[2], q_empty[2];
     uint32_t scratch[kFewThreads / 32];
     PagedRun<kFewShift, kFewItem> run;
-    uint32_t bad[kStages];                      // the tile lies on an entry that is no page
+    int32_t bad[kStages];                       // the tile's first key that lies on an entry that is no page; kNoKey: all its entries are pages
     volatile uint32_t failed;
 };
 
@@ -109,11 +110,11 @@ __device__ __forceinline__ void few_load_tile(Smem* sm, int stage, const CUtenso
     const bool load = lane < 2 * pages && key < g.w.len && !A.inject_skip_loads, is_v = lane >= pages;
     const uint32_t loads = __popc(__ballot_sync(0xffffffffu, load)), bad = __ballot_sync(0xffffffffu, load && entry < 0);
     if (lane == 0) {
-        sm->bad[stage] = bad;
+        sm->bad[stage] = bad != 0u ? j * kFewKeys + ((__ffs(bad) - 1) & (pages - 1)) * box : kNoKey;
         ptx::mbar_arrive_expect_tx(&sm->full[stage], (A.inject_skip_loads ? 1u : loads) * static_cast<uint32_t>(box) * 256u);
     }
     __syncwarp();
-    if (load)       // a bad entry marks the tile; page 0 is there
+    if (load)       // in the place of a bad entry comes page 0, which is there
         tma_load_page((is_v ? sm->v[stage] : sm->k[stage]) + row * 256, is_v ? &mv : &mk, (key & (P - 1)) >> 3,
                       max(entry, 0) * (is_v ? A.v_page_step : A.k_page_step) + g.head * (is_v ? A.v_head_step : A.k_head_step), &sm->full[stage]);
 }
@@ -228,6 +229,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
         const int limit[2] = {paged_limit(g, (row0 + (lane >> 2)) / A.G), paged_limit(g, (row0 + 8 + (lane >> 2)) / A.G)};
         const int fewest = paged_limit(g, 0);            // keys that every row sees
         const bool idle = row0 >= g.tokens * A.G;        // no rows of the tile for this warp
+        int bad = kNoKey;                                // the first key of those so far that lies on no page: rows that see it are NaN, and no others
 
         for (int j = g.j0; j < g.j1; ++j, ++tile) {
             if ((tile & 1u) != group) continue;
@@ -238,8 +240,9 @@ paged_few_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
                 if (lane == 0) ptx::mbar_arrive(&sm->empty[stage]);
                 continue;
             }
-            nan = nan || sm->bad[stage] != 0u;
+            bad = min(bad, sm->bad[stage]);
             const int key0 = j * kFewKeys + sub;
+            const int values = min(g.w.len, bad);        // keys whose values there are
             float s[2 * kWide][4];
 #pragma unroll
             for (int n = 0; n < 2 * kWide; ++n)
@@ -305,10 +308,10 @@ paged_few_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
                 // 2^-8 or 2^-11 of each, its sum is kept unrounded)
                 const uint32_t p[4] = {Pack2<T>::round(s[2 * h][0], s[2 * h][1]), Pack2<T>::round(s[2 * h][2], s[2 * h][3]),
                                        Pack2<T>::round(s[2 * h + 1][0], s[2 * h + 1][1]), Pack2<T>::round(s[2 * h + 1][2], s[2 * h + 1][3])};
-                // rows of V past the sequence hold whatever the page held, or what an earlier tile left: 0 times that has to be 0
-                const int key = key0 + 16 * h, valid = g.w.len - key - 2 * (lane & 3);
+                // rows of V past the sequence, or on no page, hold whatever some page held, or what an earlier tile left: 0 times that has to be 0
+                const int key = key0 + 16 * h, valid = values - key - 2 * (lane & 3);
                 const uint32_t keep0 = valid >= 2 ? 0xffffffffu : valid == 1 ? 0xffffu : 0u, keep1 = valid >= 10 ? 0xffffffffu : valid == 9 ? 0xffffu : 0u;
-                const bool inside = key + 16 <= g.w.len;
+                const bool inside = key + 16 <= values;
 #pragma unroll
                 for (int n = 0; n < 8; ++n) {
                     const uint32_t c = 2 * n + (lane >> 4);
@@ -332,7 +335,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
             float& x = l[i];
             x += __shfl_xor_sync(0xffffffffu, x, 1);
             x += __shfl_xor_sync(0xffffffffu, x, 2);
-            if (nan) x = __uint_as_float(0x7fc00000u);
+            if (nan || limit[i] > bad) x = __uint_as_float(0x7fc00000u);
             if ((lane & 3) == 0) sm->join_ml[peer][row0 + 8 * i + (lane >> 2)] = make_float2(m[i], x);
         }
         few_bar();

@@ -301,3 +301,48 @@ def test_nothing_to_do():
     for cu in ([0, 0], [5, 2], [-3, 1], [2, 9]):                 # no new tokens, and prefix sums that are none of the step's: nothing is written
         binding.efq_paged_attention_fwd(p.d_q, p.d_k_cache, p.d_v_cache, p.d_table, torch.tensor(cu, dtype=torch.int32, device="cuda"), p.d_seq_lens, 3, o=o)
         assert (o == 7.0).all(), cu
+
+
+def _page_zero_is_nan(p):
+    """Moves what page 0 holds to a free page: what a kernel might read in the place of a page that is none is NaN."""
+    free = next(i for i in range(1, p.d_k_cache.shape[0]) if not (p.d_table == i).any())
+    for c in (p.d_k_cache, p.d_v_cache):
+        c[free] = c[0]
+        c[0] = math.nan
+    p.d_table[p.d_table == 0] = free
+
+
+@pytest.mark.parametrize("n,Hq,Hkv", [(2, 4, 2), (4, 4, 1), (5, 8, 2), (8, 8, 2), (7, 3, 1), (16, 2, 2), (32, 1, 1)])
+@pytest.mark.parametrize("page", [16, 32, 64, 256])
+def test_a_last_page_that_is_none_is_for_the_tokens_that_see_it(n, Hq, Hkv, page):
+    """Tokens of a draft that lie before the page keep their results, to the bit, whichever kernel the announced length chooses."""
+    for m in (page * 3 + 1, page * 3 + (n + 1) // 2, page * 5 + n - 1):
+        p = Paged([(n, m), (1, 50)], Hq, Hkv, page, seed=21)
+        _page_zero_is_nan(p)
+        table = p.d_table.clone()
+        at = (m - 1) // page
+        table[0, at] = -1
+        sees = torch.zeros(p.total, dtype=torch.bool, device="cuda")
+        sees[max(0, at * page - (m - n)):n] = True              # token i sees m - n + i + 1 keys
+        for max_q in (n, 4000):
+            for causal in (True, False):
+                want, want_lse = _run(p, causal, max_q=max_q)
+                assert torch.isfinite(want).all()
+                lse = torch.zeros(p.total, Hq, device="cuda")
+                o = binding.efq_paged_attention_fwd(p.d_q, p.d_k_cache, p.d_v_cache, table, p.d_cu, p.d_seq_lens, max_q, causal, lse=lse)
+                hit = sees if causal else torch.arange(p.total, device="cuda") < n
+                assert torch.isnan(o[hit]).all() and torch.isnan(lse[hit]).all()
+                assert torch.equal(o[~hit], want[~hit]) and torch.equal(lse[~hit], want_lse[~hit])
+
+
+@pytest.mark.parametrize("n,Hq,Hkv", [(1, 8, 2), (5, 8, 2), (32, 1, 1), (40, 8, 2)])
+def test_a_page_that_is_none_inside_a_long_context(n, Hq, Hkv):
+    """One of many parts of a context lies on it: all tokens behind it are NaN, other sequences are as they were."""
+    p = Paged([(3, 700), (n, 20000), (1, 900)], Hq, Hkv, 16, seed=25)
+    want, want_lse = _run(p)
+    for at in (0, 3, 617, 1240):
+        table = p.d_table.clone()
+        table[1, at] = p.d_k_cache.shape[0] + 5
+        o = torch.zeros_like(want)
+        binding.efq_paged_attention_fwd(p.d_q, p.d_k_cache, p.d_v_cache, table, p.d_cu, p.d_seq_lens, p.max_q, o=o)
+        assert torch.isnan(o[3:3 + n]).all() and torch.equal(o[:3], want[:3]) and torch.equal(o[3 + n:], want[3 + n:]), at
