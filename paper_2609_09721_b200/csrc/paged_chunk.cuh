@@ -32,6 +32,9 @@ constexpr uint32_t kChunkColS = 0, kChunkColO = 256;           // + 128 for the 
 // log2: probabilities stay below 2^14 (fp16 ends at 2^16), sums below 2^14 times the keys.  Scores that spread as under outlier channels: 2048 tokens on
 // 32768 884 us with 8, 874 with 14, a mixed batch 274 and 271.
 constexpr float kSlack = 14.0f;
+// A maximum is a rounded product, a probability's argument a fused one: the two differ by up to half a step of the maximum.  That is a factor which all
+// of a row's probabilities have in common, up to 2^(1/2) here; beyond, where it would overflow or leave nothing, the scores are rounded too.
+constexpr float kFar = 8388608.0f;                             // 2^23
 
 // A segment of the run, as the warps that load tell it to the others: found out once, since the code of the walk is run rarely and not at hand when it is
 // (each of the others walking for itself: 3300 clocks between two segments).  Of [2] one for each half.
@@ -499,7 +502,14 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
                 for (int q = 0; q < 8; ++q) top[q] = max3(top[q], s[120 + q], top[q]);
                 const float mx = max3(max3(top[0], top[1], top[2]), max3(top[3], top[4], top[5]), max3(top[6], top[7], top[7])) * A.scale_log2;
                 const bool grew = !(mx <= m + kSlack);        // also a NaN
-                if (__any_sync(0xffffffffu, grew)) {
+                const bool far = fabsf(mx) > kFar && fabsf(mx) < INFINITY;
+                float scale = A.scale_log2;
+                if (__any_sync(0xffffffffu, grew || far)) {
+                    if (__any_sync(0xffffffffu, far)) {
+#pragma unroll
+                        for (int c = 0; c < 128; ++c) s[c] *= scale;
+                        scale = 1.0f;
+                    }
                     const float alpha = grew ? (m == -INFINITY ? 0.0f : paged_exp2(m - mx)) : 1.0f;
                     if (grew) m = mx < INFINITY ? mx : __uint_as_float(0x7fc00000u);      // an infinite score makes a row of NaN, as inf - inf does
                     l *= alpha;
@@ -517,7 +527,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
                     }
                 }
                 const float base = m == -INFINITY ? 0.0f : m;        // nothing visible yet: every exponential is 2^-inf = 0
-                const float2 scale2 = make_float2(A.scale_log2, A.scale_log2), minus2 = make_float2(-base, -base);
+                const float2 scale2 = make_float2(scale, scale), minus2 = make_float2(-base, -base);
                 float2 sum2[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {

@@ -346,3 +346,36 @@ def test_a_page_that_is_none_inside_a_long_context(n, Hq, Hkv):
         o = torch.zeros_like(want)
         binding.efq_paged_attention_fwd(p.d_q, p.d_k_cache, p.d_v_cache, table, p.d_cu, p.d_seq_lens, p.max_q, o=o)
         assert torch.isnan(o[3:3 + n]).all() and torch.equal(o[:3], want[:3]) and torch.equal(o[3 + n:], want[3 + n:]), at
+
+
+@pytest.mark.parametrize("dtype,size", [(torch.float16, 4.0), (torch.float16, 4096.0), (torch.float16, 30000.0), (torch.bfloat16, 2.0 ** 16), (torch.bfloat16, 2.0 ** 40)])
+@pytest.mark.parametrize("max_q", [1, 8, 1000])
+def test_scores_whose_steps_are_large(dtype, size, max_q):
+    """Scores up to 2^87, between which FP32 has steps of 2^64: each row has one key far above the others, whose value it gets, and lse is its score."""
+    n, m = 40, 700
+    p = Paged([(n, m)], 4, 2, 16, dtype, seed=26, hot=0)
+    g = torch.Generator().manual_seed(2)
+    sign = torch.randint(0, 2, (n, 4, D), generator=g).mul(2).sub(1).float()
+    best = torch.randint(0, m - n, (n, 2), generator=g)
+    k = torch.zeros(m, 2, D)
+    # token t of heads 2 h and 2 h + 1 agrees in all channels with its own key and in some with those of others
+    sign[:, 1::2] = sign[:, ::2]
+    for t in range(n):
+        for h in range(2):
+            k[best[t, h], h] = size * 1.1 * sign[t, 2 * h]
+    k = k.to(dtype)
+    q = (size * 1.3 * sign).to(dtype)
+    at, slot = torch.arange(m) // 16, torch.arange(m) % 16
+    p.d_k_cache[p.table[0].long()[at].cuda(), :, slot.cuda()] = k.cuda()
+    p.d_q.copy_(q)
+    o, lse = _run(p, max_q=max_q)
+    scores = torch.einsum("thd,mhd->thm", q.double(), k.double().repeat_interleave(2, 1)) / math.sqrt(D)
+    top, key = scores.max(-1)
+    rest = scores.scatter(-1, key[..., None], -math.inf).amax(-1)
+    clear = top - rest > 40 + math.log(m)                        # what the others weigh together is less than 2^-57
+    assert clear.float().mean() > 0.7
+    want = torch.stack([p.v[0][key[:, h], h // 2] for h in range(4)], 1)
+    # the weight of the key is 1 up to FP32 sums: its value comes out as it is
+    assert torch.equal(o.cpu()[clear], want[clear])
+    # a sum of 128 products: 8 steps of up to 2^-22 of it, and two roundings of 2^-24
+    assert float(((lse.cpu().double() - top).abs() / top)[clear].max()) <= 2.0 ** -18
