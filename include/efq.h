@@ -378,7 +378,7 @@ efq_status_t efq_paged_append(const efq_rows_t* k, const efq_rows_t* v, const ef
  *   workspace  device, 256-byte aligned, >= efq_paged_attention_workspace_bytes(...); its contents need not be kept and need no
  *           preparation.  Calls that may overlap (other streams, graphs that run beside one another) need one each.
  * Scores, maxima, sums and the output's accumulator are FP32, the probabilities of a tile are rounded to the elements' type for the product
- * with V.  A token that sees no key gets a row of zeros and lse = -inf.  Rows behind cu_seqlens[n_seqs] are left alone.  What lies in the pages
+ * with V (fp16: to 11 bits from 2^-20 of the row's largest one on, to 2^-31 of that below).  A token that sees no key gets a row of zeros and lse = -inf.  Rows behind cu_seqlens[n_seqs] are left alone.  What lies in the pages
  * behind a sequence's last token does not matter; an infinity or NaN in a value of the sequence makes NaN of its channel in
  * every row of the 128 x 128 tiles that hold it.  Rows are NaN that see a key for which the page table names no page (an entry below
  * zero or from n_pages on), those of a sequence longer than max_pages * page_size, and in blocks in which a bounded device-side wait expired.

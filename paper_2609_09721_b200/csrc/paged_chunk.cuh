@@ -6,7 +6,7 @@
 // of V past a sequence.  While the softmax warps of one half are busy, the tensor core has the other half's products: per half and tile Q K^T (both
 // operands in shared memory), then P V (P from tensor memory).
 //   - A thread has a row, so maxima and sums need no other thread.  The output is rescaled in tensor memory by the same threads,
-//     only when a row's maximum has grown by more than 2^14 (kSlack); the sum refers to the same maximum, so the result is exact.  When
+//     only when a row's maximum has grown by more than 2^14 (2^9 in fp16, kSlack); the sum refers to the same maximum, so the result is exact.  When
 //     the scores of a tile are there, the product of the tile before has ended (the tensor core works in order), so nobody waits for it.
 //   - K and V come through one ring of 32 KB slots, pages by TMA; 64 KB hold Q.
 //   - The CTAs of a head read the same tiles at about the same time, so that L2 has them once and not every CTA's own part of a long context.
@@ -29,9 +29,13 @@ constexpr int kChunkThreads = 384;
 constexpr int kChunkSlots = 5;
 constexpr int kChunkPart = kChunkKeys * 128;                   // bytes of 64 channels of 128 rows
 constexpr uint32_t kChunkColS = 0, kChunkColO = 256;           // + 128 for the second half
-// log2: probabilities stay below 2^14 (fp16 ends at 2^16), sums below 2^14 times the keys.  Scores that spread as under outlier channels: 2048 tokens on
-// 32768 884 us with 8, 874 with 14, a mixed batch 274 and 271.
-constexpr float kSlack = 14.0f;
+// log2: how far a row's maximum may grow before the output is rescaled; with kChunkRaise, what the probabilities stay below (fp16 ends at 2^16), sums below
+// that times the keys.  Scores that spread as under outlier channels: 2048 tokens on 32768 884 us with 8, 874 with 14, a mixed batch 274 and 271.
+// fp16 shares the 15 powers that it has above 1 between the two: probabilities down to 2^-20 of the row's maximum keep all their bits, smaller ones are
+// off by up to 2^-31 of it, so that a million of them are less than a rounding.  fp16, raised by 0 with a slack of 14, by 6 with 9, 8 with 7 and 10 with 5:
+// 2048 tokens on 32768 901, 927, 949 and 980 us, 300 on 9000 56.9, 58.8, 61.3 and 65.6, 64 chunks of 300 on 600 234, 240, 245 and 255.
+template <typename T> constexpr float kChunkRaise = kNarrowExponent<T> ? 6.0f : 0.0f;
+template <typename T> constexpr float kSlack = kNarrowExponent<T> ? 9.0f : 14.0f;
 // A maximum is a rounded product, a probability's argument a fused one: the two differ by up to half a step of the maximum.  That is a factor which all
 // of a row's probabilities have in common, up to 2^(1/2) here; beyond, where it would overflow or leave nothing, the scores are rounded too.
 constexpr float kFar = 8388608.0f;                             // 2^23
@@ -93,8 +97,8 @@ __device__ __forceinline__ float max3(float a, float b, float c)
     asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
 }
-// 2^x for x <= 14 on the FMA pipe: x = n + f with n the nearest integer, 1 + f q(f) with q of degree 3 fitted to the smallest relative error on
-// [-1/2, 1/2] (least squares, reweighted until the error is level: 2.9e-6, a thousandth of what rounding the probability costs), n added
+// 2^x for x <= 15 on the FMA pipe: x = n + f with n the nearest integer, 1 + f q(f) with q of degree 3 fitted to the smallest relative error on
+// [-1/2, 1/2] (least squares, reweighted until the error is level: 2.9e-6, a 1300th of what rounding the probability may cost in bf16, a 160th in fp16), n added
 // to the exponent.  Below -127 the result is 0, exactly: f = 0 there and the exponent field is empty.  NaN is not kept.
 __device__ __forceinline__ float2 poly_exp2(float2 x)
 {
@@ -501,7 +505,8 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
 #pragma unroll
                 for (int q = 0; q < 8; ++q) top[q] = max3(top[q], s[120 + q], top[q]);
                 const float mx = max3(max3(top[0], top[1], top[2]), max3(top[3], top[4], top[5]), max3(top[6], top[7], top[7])) * A.scale_log2;
-                const bool grew = !(mx <= m + kSlack);        // also a NaN
+                const float reference = paged_reference(mx, kChunkRaise<T>);
+                const bool grew = !(reference <= __fadd_rd(m, kSlack<T>));        // also a NaN; a step of m may be more than the slack
                 const bool far = fabsf(mx) > kFar && fabsf(mx) < INFINITY;
                 float scale = A.scale_log2;
                 if (__any_sync(0xffffffffu, grew || far)) {
@@ -510,8 +515,8 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
                         for (int c = 0; c < 128; ++c) s[c] *= scale;
                         scale = 1.0f;
                     }
-                    const float alpha = grew ? (m == -INFINITY ? 0.0f : paged_exp2(m - mx)) : 1.0f;
-                    if (grew) m = mx < INFINITY ? mx : __uint_as_float(0x7fc00000u);      // an infinite score makes a row of NaN, as inf - inf does
+                    const float alpha = grew ? (m == -INFINITY ? 0.0f : paged_exp2(m - reference)) : 1.0f;
+                    if (grew) m = reference < INFINITY ? reference : __uint_as_float(0x7fc00000u);      // an infinite score makes a row of NaN, as inf - inf does
                     l *= alpha;
                     if (j > j0) {
 #pragma unroll 1
@@ -544,7 +549,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
                         // a quarter of the exponentials by polynomial (an eighth: 946 us and 889, three eighths: 903)
                         y = c % 4 == 3 ? poly_exp2(y) : make_float2(paged_exp2(y.x), paged_exp2(y.y));
                         sum2[c & 1] = add2(sum2[c & 1], y);
-                        // rounded once, to the elements' type (half a step of 2^-8 or 2^-11 of each); the sum is kept unrounded
+                        // rounded once, to the elements' type (off by up to 2^-8 or 2^-11 of each, and kChunkRaise); the sum is kept unrounded
                         p[c] = Pack2<T>::round(y.x, y.y);
                     }
                     tmem_st16(s_col + 16 * q, p);        // over scores that have been read

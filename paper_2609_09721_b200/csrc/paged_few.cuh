@@ -23,6 +23,8 @@ constexpr int kFewThreads = (kFewWarps + 1) * 32;
 constexpr int kFewRows = 16;                     // of a product; a query tile has 16 or 32 rows
 constexpr int kFewRowPad = 136;                 // floats of a row in the join: rows start 8 banks apart
 constexpr int kNoKey = 0x7fffffff;
+// log2 of the largest probability.  fp16: those down to 2^-29 of the row's maximum keep all their bits, smaller ones are off by up to 2^-40 of it.
+template <typename T> constexpr float kFewRaise = kNarrowExponent<T> ? 15.0f : 0.0f;
 
 template <int kRows>
 struct __align__(1024) FewSmem {
@@ -277,7 +279,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
             for (int i = 0; i < 2; ++i) {
                 top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
                 top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
-                top[i] = fmaxf(top[i], m[i]);
+                top[i] = fmaxf(paged_reference(top[i], kFewRaise<T>), m[i]);
                 base[i] = top[i] == -INFINITY ? 0.0f : top[i];        // nothing visible yet: every exponential is 2^-inf = 0
                 grew = grew || top[i] > m[i];
             }
@@ -304,8 +306,8 @@ paged_few_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
             const uint32_t vb = ptx::smem_u32(sm->v[stage]) + v_at;
 #pragma unroll
             for (int h = 0; h < kWide; ++h) {
-                // the scores' layout is that of the left operand: probabilities are rounded once, to the elements' type (half a step of
-                // 2^-8 or 2^-11 of each, its sum is kept unrounded)
+                // the scores' layout is that of the left operand: probabilities are rounded once, to the elements' type (off by up to 2^-8 or
+                // 2^-11 of each, and kFewRaise; their sum is kept unrounded)
                 const uint32_t p[4] = {Pack2<T>::round(s[2 * h][0], s[2 * h][1]), Pack2<T>::round(s[2 * h][2], s[2 * h][3]),
                                        Pack2<T>::round(s[2 * h + 1][0], s[2 * h + 1][1]), Pack2<T>::round(s[2 * h + 1][2], s[2 * h + 1][3])};
                 // rows of V past the sequence, or on no page, hold whatever some page held, or what an earlier tile left: 0 times that has to be 0

@@ -126,6 +126,12 @@ __device__ __forceinline__ float paged_exp2(float x)
     return y;
 }
 
+// The exponent of a row's probabilities for the product with V is raised by 2^raise over what it is under the row's maximum: fp16 is exact to half a
+// step of 2^-11 from 2^-14 on only, to 2^-25 below, and ends at 65504.  What the maximum is kept as is lower by as much, so sums, parts and lse need to
+// know nothing of it.  Rounded up, so that a probability is at most 2^raise wherever the maximum lies.
+template <typename T> constexpr bool kNarrowExponent = sizeof(T) == 2 && __is_same(T, __half);
+__device__ __forceinline__ float paged_reference(float top, float raise) { return raise == 0.0f ? top : __fadd_ru(top, -raise); }
+
 constexpr float kLn2 = 0.69314718055994530942f;
 
 }  // namespace efq

@@ -379,3 +379,51 @@ def test_scores_whose_steps_are_large(dtype, size, max_q):
     assert torch.equal(o.cpu()[clear], want[clear])
     # a sum of 128 products: 8 steps of up to 2^-22 of it, and two roundings of 2^-24
     assert float(((lse.cpu().double() - top).abs() / top)[clear].max()) <= 2.0 ** -18
+
+
+@pytest.mark.parametrize("n,Hq,Hkv,m", [(1, 1, 1, 65537), (1, 32, 8, 4097), (5, 8, 2, 131072), (32, 1, 1, 20000), (40, 2, 1, 65576), (300, 2, 1, 131372), (130, 8, 2, 2000),
+                                         (1, 160, 160, 4097), (3, 160, 40, 4099), (24, 150, 150, 4119), (300, 40, 40, 4396), (40, 192, 48, 4136)])
+@pytest.mark.parametrize("below", [12.25, 18.25, 25.25])
+def test_a_key_above_a_long_flat_tail(n, Hq, Hkv, m, below):
+    """The first key's score is 2^below times the weight of each of the others, which in fp16 would be a number without all its bits, or 0: the
+    values of the many others have to be in the output all the same, also where the first key's is 0."""
+    for dtype in (torch.float16, torch.bfloat16):
+        p = Paged([(n, m)], Hq, Hkv, 64, dtype, seed=22, hot=0)
+        g = torch.Generator().manual_seed(1)
+        p.k[0] = torch.zeros(m, Hkv, D, dtype=dtype)
+        p.k[0][0, :, 0] = below
+        v = torch.rand(m, Hkv, D, generator=g) + 0.5
+        v[0, :, ::2] = 0.0
+        p.v[0] = v.to(dtype)
+        at, slot = p.table[0].long()[torch.arange(m) // 64].cuda(), (torch.arange(m) % 64).cuda()
+        p.d_k_cache[at, :, slot], p.d_v_cache[at, :, slot] = p.k[0].cuda(), p.v[0].cuda()
+        p.d_q.zero_()
+        p.d_q[..., 0] = 1.0
+        o, lse = _run(p, scale=math.log(2.0))
+        want, want_lse, tol, lse_tol = p.attention(True, math.log(2.0))
+        # beside what other values of the tests may be off by: a probability below 2^-20 of the row's maximum is rounded to a step of 2^-30 of it
+        tail = 2.0 ** -31 * p.v[0].double().sum(0).max() if dtype == torch.float16 else 0.0
+        assert float(((o.double() - want).abs() - tol - tail).max()) <= 0.0
+        assert float(((lse.double() - want_lse).abs() - lse_tol).max()) <= 0.0
+
+
+@pytest.mark.parametrize("grows", [2, 4, 6, 8, 14, 16])
+@pytest.mark.parametrize("max_q", [1, 1000])
+def test_a_maximum_that_grows_by_little_far_from_zero(grows, max_q):
+    """Scores near 2^25 / log2(e), where FP32 has steps of 2 in units of log2, and one in a later tile that is 2^grows as heavy: what is kept of the maximum
+    must not be rounded to where the probability is more than fp16 holds."""
+    n, m = 40, 700
+    p = Paged([(n, m)], 2, 2, 16, torch.float16, seed=27, hot=0)
+    k = torch.zeros(m, 2, D)
+    k[:, :, 0], k[:, :, 1] = 16384.0, -64.0 - 32.0               # the others weigh 2^-32 and less of the first
+    k[0, :, 1], k[300, :, 1] = -64.0, -64.0 + grows
+    p.k[0] = k.half()
+    at, slot = p.table[0].long()[torch.arange(m) // 16].cuda(), (torch.arange(m) % 16).cuda()
+    p.d_k_cache[at, :, slot] = p.k[0].cuda()
+    p.d_q.zero_()
+    p.d_q[..., 0], p.d_q[..., 1] = 2048.0, 1.0
+    o, _ = _run(p, scale=math.log(2.0), max_q=max_q)
+    v, w = p.v[0].double(), 2.0 ** grows
+    near = ((v[0] + w * v[300]) / (1 + w))[None].cuda()          # the steps of 2 are exact here: probabilities and the output are rounded once
+    bound = 2.0 ** -11 * ((v[0].abs() + w * v[300].abs()) / (1 + w)).cuda() * 2.1 + 700 * 2.0 ** -32 * 4
+    assert float(((o.double() - near).abs() - bound).max()) <= 0.0
