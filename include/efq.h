@@ -341,7 +341,8 @@ efq_status_t efq_rotary(const efq_rows_t* q, const efq_rows_t* k, const int32_t*
  * recorded graph follows them from replay to replay.
  *   k, v         [n_pages, n_heads, page_size, 128], strides in elements (a token-major cache is one with other strides)
  *   page_size    a power of two from 16 to 4096
- *   max_pages    entries of a row of page_table; those behind a sequence's last page are not read */
+ *   max_pages    entries of a row of page_table; those behind a sequence's last page are not read; max_pages * page_size is at most
+ *                2^31 - 256 (UNSUPPORTED otherwise) */
 typedef struct {
     void *k, *v;
     int64_t k_page, k_head, k_token;

@@ -42,7 +42,8 @@ inline efq_status_t check_paged(const efq_paged_t& c, int d, int dtype)
     if (c.n_pages <= 0 || c.n_heads <= 0 || c.max_pages <= 0 || c.n_seqs < 0 || c.table_stride < 0) return EFQ_ERR_INVALID_ARG;
     if (dtype != EFQ_BF16 && dtype != EFQ_FP16) return EFQ_ERR_UNSUPPORTED;
     if (d != kPagedD || c.page_size < 16 || c.page_size > 4096 || (c.page_size & (c.page_size - 1)) != 0) return EFQ_ERR_UNSUPPORTED;
-    if (static_cast<int64_t>(c.max_pages) * c.page_size >= (1ll << 31)) return EFQ_ERR_UNSUPPORTED;      // 32-bit indices of a sequence's tokens
+    // 32-bit indices of a sequence's tokens, up to the end of a tile of 128 of them that the last one lies in
+    if (static_cast<int64_t>(c.max_pages) * c.page_size > (1ll << 31) - 256) return EFQ_ERR_UNSUPPORTED;
     if (!aligned_ints(c.page_table) || !aligned_ints(c.cu_seqlens) || !aligned_ints(c.seq_lens)) return EFQ_ERR_ALIGNMENT;
     if (c.k_page < 0 || c.k_head < 0 || c.k_token < 0 || c.v_page < 0 || c.v_head < 0 || c.v_token < 0) return EFQ_ERR_INVALID_ARG;
     if (!aligned_rows(c.k, c.k_page, c.k_head, c.k_token) || !aligned_rows(c.v, c.v_page, c.v_head, c.v_token)) return EFQ_ERR_ALIGNMENT;

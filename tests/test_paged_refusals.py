@@ -240,3 +240,15 @@ def test_more_heads_than_32_bits_are_refused():
     most = 2**31 - 1
     assert _rotary(_rows(heads=most), _rows(heads=most), rotation=_rotation()) == UNSUPPORTED
     assert _append(_rows(heads=2), _rows(heads=2), _rows(heads=most), cache=_cache()) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("page", [16, 32, 64, 128, 4096])
+def test_tokens_of_a_sequence_end_a_tile_before_31_bits(page):
+    """The kernels' keys are 32-bit numbers up to the end of the last tile of 128: a page table with room for more than 2^31 - 256 tokens is refused."""
+    most = (2**31 - 256) // page
+    for max_pages in (2**31 // page - 1, most + 1):
+        if max_pages * page > 2**31 - 256:
+            bad = _cache(page_size=page, max_pages=max_pages, n_seqs=1)
+            assert _attention(_rows(), bad) == UNSUPPORTED and _append(_rows(heads=2), _rows(heads=2), cache=bad) == UNSUPPORTED, max_pages
+    good = _cache(page_size=page, max_pages=most, n_seqs=0)
+    assert _attention(_rows(), good) == OK and _append(_rows(heads=2), _rows(heads=2), cache=good) == OK
