@@ -267,8 +267,8 @@ efq_status_t paged_attention(const efq_rows_t* q, float* lse, int64_t total, int
     const PagedPlan plan = plan_paged(group_rows);
     const bool many = plan.rows > 2 * kFewRows;
     const int step = many ? kChunkRows / G * 2 : plan.rows / G;         // new tokens of a query tile
-    if (paged_most_units(total, cache->n_seqs, static_cast<int64_t>(cache->max_pages) * cache->page_size, cache->n_heads, step, many ? kChunkShift : kFewShift,
-                         many ? kChunkItem : kFewItem) >= (1ll << 31))
+    if (paged_too_many_units(total, cache->n_seqs, static_cast<int64_t>(cache->max_pages) * cache->page_size, cache->n_heads, step, many ? kChunkShift : kFewShift,
+                             many ? kChunkItem : kFewItem))
         return EFQ_ERR_UNSUPPORTED;
     if (!workspace || workspace_bytes < plan.total) return EFQ_ERR_WORKSPACE;
     if (reinterpret_cast<uintptr_t>(workspace) & 255u) return EFQ_ERR_ALIGNMENT;

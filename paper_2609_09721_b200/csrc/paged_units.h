@@ -18,7 +18,7 @@
 
 namespace efq {
 
-// All numbers of units fit 31 bits: a step that might have more is refused (paged_most_units()).  The search for a CTA's run stands before its
+// All numbers of units fit 31 bits: a step that might have more is refused (paged_too_many_units()).  The search for a CTA's run stands before its
 // first load, and it is the instructions that cost there, fetched for the first time; 64 bits made three of one.
 
 // sum over i < n of floor((b + a i) / 2^shift), a > 0, which fits 32 bits.  The terms grow by a fixed amount from one period of
@@ -118,11 +118,11 @@ struct PagedShares {
         return unit < wide ? unit / (each + 1u) : more + (unit - wide) / each;
     }
 };
-// More units than a step can have: `tokens` new ones in n_seqs sequences of at most `keys` keys.
-EFQ_HD int64_t paged_most_units(int64_t tokens, int n_seqs, int64_t keys, int heads, int step, int shift, int item)
+// Whether a step may have more units than 31 bits hold: `tokens` new ones (below 2^31) in n_seqs sequences of at most `keys` keys (below 2^31).
+EFQ_HD bool paged_too_many_units(int64_t tokens, int n_seqs, int64_t keys, int heads, int step, int shift, int item)
 {
-    const int64_t tiles = tokens / step + n_seqs, of_tile = (keys >> shift) + 1 + item;
-    return tiles > (int64_t{1} << 40) / of_tile ? int64_t{1} << 62 : tiles * of_tile * heads;
+    const int64_t tiles = tokens / step + n_seqs, of_tile = (keys >> shift) + 1 + item;         // below 2^32 and 2^31: no product of three
+    return tiles > ((int64_t{1} << 31) - 1) / of_tile / heads;
 }
 // The run of CTA c, which begins at unit `off` of sequence s; paged_begin_tile() has to follow with the query tile that holds unit run->unit of
 // the head.

@@ -252,3 +252,10 @@ def test_tokens_of_a_sequence_end_a_tile_before_31_bits(page):
             assert _attention(_rows(), bad) == UNSUPPORTED and _append(_rows(heads=2), _rows(heads=2), cache=bad) == UNSUPPORTED, max_pages
     good = _cache(page_size=page, max_pages=most, n_seqs=0)
     assert _attention(_rows(), good) == OK and _append(_rows(heads=2), _rows(heads=2), cache=good) == OK
+
+
+@pytest.mark.parametrize("heads", [2**24, 2**25, 2**27 + 3, 2**30, 2**31 - 1])
+def test_steps_of_more_key_tiles_than_31_bits_are_refused_for_any_number_of_heads(heads):
+    """Sequences times tiles of a context times heads are 2^63 and more here."""
+    for n_seqs in (40000 * 2**24 // heads, 50000 * 2**24 // heads, 65000 * 2**24 // heads):
+        assert _attention(_rows(heads=heads), _cache(n_heads=heads, max_pages=2**26, n_seqs=n_seqs), total=1) == UNSUPPORTED, n_seqs
