@@ -375,7 +375,7 @@ efq_status_t efq_paged_append(const efq_rows_t* k, const efq_rows_t* v, const ef
  *           a multiple of cache->n_heads, at most 128 times as many; query head h reads KV head h / (heads / n_heads)
  *   lse     NULL, or float [total, heads]: log sum_j exp(scale q k_j); what two partial contexts are joined by
  *   max_seqlen_q  the most new tokens that any sequence has: chooses the kernel.  Sequences with more are computed all the same.
- *   softmax_scale  <= 0 selects 1/sqrt(d)
+ *   softmax_scale  <= 0 selects 1/sqrt(d); NaN, or one that is infinite times 1 / ln 2: INVALID_ARG
  *   workspace  device, 256-byte aligned, >= efq_paged_attention_workspace_bytes(...); its contents need not be kept and need no
  *           preparation.  Calls that may overlap (other streams, graphs that run beside one another) need one each.
  * Scores, maxima, sums and the output's accumulator are FP32, the probabilities of a tile are rounded to the elements' type for the product

@@ -253,7 +253,9 @@ efq_status_t paged_attention(const efq_rows_t* q, float* lse, int64_t total, int
 {
     if (!q || !cache || total < 0 || max_seqlen_q < 0 || q->heads <= 0) return EFQ_ERR_INVALID_ARG;
     if (total > 0 && (!q->src || !q->dst)) return EFQ_ERR_INVALID_ARG;
-    if (!(softmax_scale == softmax_scale) || softmax_scale > 3.0e38f) return EFQ_ERR_INVALID_ARG;
+    const double scale = softmax_scale > 0.0f ? static_cast<double>(softmax_scale) : 0.08838834764831844055;
+    const float scale_log2 = static_cast<float>(scale * 1.44269504088896340736);
+    if (!(softmax_scale == softmax_scale) || scale_log2 > 3.4028234e38f) return EFQ_ERR_INVALID_ARG;      // infinite in units of log2
     const efq_status_t st = check_paged(*cache, d, dtype);
     if (st != EFQ_OK) return st;
     if (q->heads % cache->n_heads != 0) return EFQ_ERR_INVALID_ARG;
@@ -292,8 +294,7 @@ efq_status_t paged_attention(const efq_rows_t* q, float* lse, int64_t total, int
     A.G = G;
     A.causal = causal ? 1 : 0;
     A.total = static_cast<int32_t>(total);
-    const double scale = softmax_scale > 0.0f ? static_cast<double>(softmax_scale) : 0.08838834764831844055;
-    A.scale_log2 = static_cast<float>(scale * 1.44269504088896340736);
+    A.scale_log2 = scale_log2;
     A.o = static_cast<char*>(q->dst);
     A.o_token = 2 * q->dst_token;
     A.o_head = 2 * q->dst_head;

@@ -259,3 +259,10 @@ def test_steps_of_more_key_tiles_than_31_bits_are_refused_for_any_number_of_head
     """Sequences times tiles of a context times heads are 2^63 and more here."""
     for n_seqs in (40000 * 2**24 // heads, 50000 * 2**24 // heads, 65000 * 2**24 // heads):
         assert _attention(_rows(heads=heads), _cache(n_heads=heads, max_pages=2**26, n_seqs=n_seqs), total=1) == UNSUPPORTED, n_seqs
+
+
+def test_scales_that_are_infinite_in_units_of_log2_are_refused():
+    for scale in (2.4e38, 3.0e38, 3.4e38):
+        assert _attention(_rows(), _cache(), scale=scale) == INVALID, scale
+    for scale in (2.3e38, 1e-45, -1.0, float("-inf")):
+        assert _attention(_rows(), _cache(), scale=scale, total=0) == OK, scale
