@@ -382,20 +382,22 @@ efq_status_t efq_paged_append(const efq_rows_t* k, const efq_rows_t* v, const ef
  * with V (fp16: to 11 bits from 2^-20 of the row's largest one on, to 2^-31 of that below).  A token that sees no key gets a row of zeros and lse = -inf.  Rows behind cu_seqlens[n_seqs] are left alone.  What lies in the pages
  * behind a sequence's last token does not matter; an infinity or NaN in a value of the sequence makes NaN of its channel in
  * every row of the 128 x 128 tiles that hold it.  Rows are NaN that see a key for which the page table names no page (an entry below
- * zero or from n_pages on), those of a sequence longer than max_pages * page_size, and in blocks in which a bounded device-side wait expired.
+ * zero or from n_pages on), those of a sequence longer than max_pages * page_size, and in blocks in which a bounded device-side wait expired,
+ * which efq_poll_status reports too.
  * Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, WORKSPACE, ARCH, CUDA.  total == 0 or n_seqs == 0 is a valid no-op. */
 size_t efq_paged_attention_workspace_bytes(int Hq, int Hkv, int max_seqlen_q, int d);
 efq_status_t efq_paged_attention_fwd(const efq_rows_t* q, float* lse, int64_t total, int max_seqlen_q, const efq_paged_t* cache, int d,
                                      int dtype, int causal, float softmax_scale, void* workspace, size_t workspace_bytes, void* stream);
 
-/* Test hook as efq_attention_fwd_inject_timeout, for efq_paged_attention_fwd: K and V are not loaded.  The rows of `o` become NaN. */
+/* Test hook as efq_attention_fwd_inject_timeout, for efq_paged_attention_fwd: K and V are not loaded.  The rows of `o` become NaN, and
+ * efq_poll_status returns EFQ_ERR_DEVICE_TIMEOUT. */
 efq_status_t efq_paged_attention_fwd_inject_timeout(const efq_rows_t* q, float* lse, int64_t total, int max_seqlen_q, const efq_paged_t* cache,
                                                     int d, int dtype, int causal, float softmax_scale, void* workspace,
                                                     size_t workspace_bytes, void* stream);
 
-/* Synchronises `stream` and returns the device-side status word of the last forward that
- * used `workspace` (EFQ_OK, or EFQ_ERR_DEVICE_TIMEOUT if a bounded wait expired), or
- * EFQ_ERR_CUDA if the stream reports an error. */
+/* Synchronises `stream` and returns the device-side status of the last forward, dense, packed or
+ * paged, that used `workspace` (EFQ_OK, or EFQ_ERR_DEVICE_TIMEOUT if a bounded wait expired), or
+ * EFQ_ERR_CUDA if the stream reports an error.  A call that had nothing to do leaves it as it was. */
 efq_status_t efq_poll_status(void* workspace, void* stream);
 
 /* Dense FP4 tensor-pipe microbenchmark: `iters` back-to-back 128x256x64 block-scaled E2M1 MMAs per CTA on

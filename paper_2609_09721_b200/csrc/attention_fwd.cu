@@ -1534,6 +1534,15 @@ extern "C" efq_status_t efq_poll_status(void* workspace, void* stream)
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (cudaMemcpyAsync(&word, workspace, 4, cudaMemcpyDeviceToHost, s) != cudaSuccess) return EFQ_ERR_CUDA;
     if (cudaStreamSynchronize(s) != cudaSuccess) return EFQ_ERR_CUDA;
+    if (word == efq::kPagedStatus) {
+        constexpr size_t n = efq::kPagedExpired / 4 + efq::kPagedMaxCtas;
+        uint32_t words[n];
+        if (cudaMemcpyAsync(words, workspace, sizeof(words), cudaMemcpyDeviceToHost, s) != cudaSuccess) return EFQ_ERR_CUDA;
+        if (cudaStreamSynchronize(s) != cudaSuccess || words[1] > efq::kPagedMaxCtas) return EFQ_ERR_CUDA;
+        for (uint32_t c = 0; c < words[1]; ++c)
+            if (words[efq::kPagedExpired / 4 + c] != 0) return EFQ_ERR_DEVICE_TIMEOUT;
+        return EFQ_OK;
+    }
     return word == 0 ? EFQ_OK : (word == EFQ_ERR_DEVICE_TIMEOUT ? EFQ_ERR_DEVICE_TIMEOUT : EFQ_ERR_CUDA);
 }
 

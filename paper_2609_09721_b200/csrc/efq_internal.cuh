@@ -61,6 +61,13 @@ struct ItemGroup {
 };
 struct ItemDesc;
 
+// A workspace's first word is the status of the last call that used it.  A paged call leaves the words of its blocks instead, so that none has to be
+// cleared before the blocks run or joined behind them: kPagedStatus, their number, and from kPagedExpired bytes on a word of each, not 0 if a wait of the
+// block has expired.
+constexpr uint32_t kPagedStatus = 0x70616765u;
+constexpr size_t kPagedExpired = 256;
+constexpr int kPagedMaxCtas = 256;       // of the kernels that take the key tiles; the workspace has room for the parts of as many
+
 // SMs of a device, asked for once (0: no such device)
 int sm_count(int dev);
 

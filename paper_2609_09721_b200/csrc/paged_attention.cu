@@ -11,8 +11,6 @@
 namespace efq {
 namespace {
 
-constexpr int kMaxCtas = 256;            // of the first kernel; the workspace has room for the parts of as many
-
 // Joins the parts of the query tiles that span CTAs.  blockIdx.x: the CTA that ended the tile, blockIdx.y: a row of it (and further ones where
 // a tile has more).  Eight warps take every eighth part each, two of them at a time, a lane four channels: bound by latency, so maxima, sums and
 // outputs of as many parts are asked for at once.  One long context may leave a part in every CTA: one head of 60000 keys 15.0 us with eight
@@ -203,16 +201,17 @@ efq_status_t encode_cache(CUtensorMap* map, int dtype, const void* base, int64_t
 // 5000 74.2 and 74.5, one of 8 on 8000 17.5 and 22.9, 60 of 8 on 700 53.5 and 49.9, 60 of 5 on 700 48.7 and 50.4.
 struct PagedPlan {
     int rows;                            // of a query tile
-    size_t ml, records, total;
+    size_t parts, ml, records, total;    // behind the words of the status
 };
 PagedPlan plan_paged(int64_t group_rows)
 {
     PagedPlan p;
     p.rows = group_rows <= kFewRows ? kFewRows : group_rows <= 2 * kFewRows ? 2 * kFewRows : 2 * kChunkRows;
     const int room = p.rows > kFewRows ? 2 * kChunkRows : kFewRows;         // one size for all that is not a decode step
-    p.ml = static_cast<size_t>(2 * kMaxCtas) * room * kPagedD * 4;
-    p.records = p.ml + static_cast<size_t>(2 * kMaxCtas) * room * sizeof(float2);
-    p.total = p.records + kMaxCtas * sizeof(PagedRecord);       // records on 16 bytes: 2 * kMaxCtas * rows is a multiple of 8
+    p.parts = kPagedExpired + kPagedMaxCtas * sizeof(uint32_t);
+    p.ml = p.parts + static_cast<size_t>(2 * kPagedMaxCtas) * room * kPagedD * 4;
+    p.records = p.ml + static_cast<size_t>(2 * kPagedMaxCtas) * room * sizeof(float2);
+    p.total = p.records + kPagedMaxCtas * sizeof(PagedRecord);       // records on 16 bytes: 2 * kPagedMaxCtas * rows is a multiple of 8
     return p;
 }
 
@@ -279,7 +278,7 @@ efq_status_t paged_attention(const efq_rows_t* q, float* lse, int64_t total, int
     if (cudaGetDevice(&dev) != cudaSuccess) return EFQ_ERR_CUDA;
     int ctas = sm_count(dev);
     if (ctas <= 0) return EFQ_ERR_CUDA;
-    if (ctas > kMaxCtas) ctas = kMaxCtas;
+    if (ctas > kPagedMaxCtas) ctas = kPagedMaxCtas;
 
     PagedArgs A{};
     A.page_table = cache->page_table;
@@ -301,7 +300,9 @@ efq_status_t paged_attention(const efq_rows_t* q, float* lse, int64_t total, int
     A.o_wide = ((reinterpret_cast<uintptr_t>(A.o) | static_cast<uintptr_t>(A.o_token) | static_cast<uintptr_t>(A.o_head)) & 31u) == 0 ? 1 : 0;
     A.lse = lse;
     char* const ws = static_cast<char*>(workspace);
-    A.part_o = reinterpret_cast<float*>(ws);
+    A.header = reinterpret_cast<uint32_t*>(ws);
+    A.expired = reinterpret_cast<uint32_t*>(ws + kPagedExpired);
+    A.part_o = reinterpret_cast<float*>(ws + plan.parts);
     A.part_ml = reinterpret_cast<float2*>(ws + plan.ml);
     A.records = reinterpret_cast<PagedRecord*>(ws + plan.records);
     A.inject_skip_loads = inject_skip_loads ? 1 : 0;

@@ -62,6 +62,7 @@ struct __align__(1024) ChunkSmem {
     PagedRun<kChunkShift, kChunkItem> run;
     uint32_t tmem_base;
     volatile uint32_t failed;
+    uint32_t* expired;                          // where the call's status has this block
 };
 
 // Registers of a softmax thread, which holds a row of scores, and of the others: together what the block is launched with, 384 x 168.  208 and 88: 2048
@@ -164,11 +165,15 @@ __device__ __forceinline__ ChunkSegment chunk_segment(const PagedSegment<kChunkS
 }
 // The wait for a segment, or for the room of one.  It goes on when another wait has expired, since the rows of the segments that are left become
 // NaN then: their warps let go of them without one, so two seconds are more than any of these waits can take.
-__device__ __forceinline__ bool chunk_segment_wait(uint64_t* bar, uint32_t parity)
+__device__ __forceinline__ bool chunk_segment_wait(uint64_t* bar, uint32_t parity, ChunkSmem* sm)
 {
     bool there = ptx::mbar_try_wait(bar, parity);
 #pragma unroll 1
     for (int i = 0; !there && i < 40000; ++i) there = ptx::mbar_try_wait_suspend(bar, parity, 50000u);
+    if (!there) {
+        sm->failed = 1u;
+        *sm->expired = 1u;
+    }
     return __all_sync(0xffffffffu, there) != 0;
 }
 
@@ -182,6 +187,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
     const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
     if (tid == 0) {
         sm->failed = 0u;
+        sm->expired = A.expired + blockIdx.x;
         for (int i = 0; i < kChunkSlots; ++i) {
             ptx::mbar_init(&sm->full[i], 1);
             ptx::mbar_init(&sm->empty[i], 2);
@@ -210,6 +216,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
     ptx::tc_fence_before_sync();
     ptx::grid_wait();
     ptx::grid_launch_next();
+    if (tid == kChunkThreads - 1) paged_begin_status(A);
     paged_find_run<kChunkThreads, kChunkShift, kChunkItem>(A, sm->scratch, &sm->run);      // barriers of the block
     ptx::tc_fence_after_sync();
     const uint32_t tmem = sm->tmem_base;
@@ -217,7 +224,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
     // the next one; false at the end of the run
     auto next = [&](ChunkSegment& d) {
         const uint32_t at = seg % kChunkSegments;
-        if (!chunk_segment_wait(&sm->seg_full[at], (seg / kChunkSegments) & 1u)) return false;
+        if (!chunk_segment_wait(&sm->seg_full[at], (seg / kChunkSegments) & 1u, sm)) return false;
         d = sm->seg[at];
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(&sm->seg_empty[at]);
@@ -240,7 +247,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
                 if (more) d = chunk_segment(g, A.step);
                 else d.j0 = -1;
                 const uint32_t at = seg % kChunkSegments;
-                if (seg >= kChunkSegments && !chunk_segment_wait(&sm->seg_empty[at], (seg / kChunkSegments - 1) & 1u)) break;
+                if (seg >= kChunkSegments && !chunk_segment_wait(&sm->seg_empty[at], (seg / kChunkSegments - 1) & 1u, sm)) break;
                 if (lane == 0) {
                     sm->seg[at] = d;
                     ptx::mbar_arrive(&sm->seg_full[at]);
@@ -472,7 +479,6 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
         const uint32_t s_col = tmem + lane_base + kChunkColS + 128 * w, o_col = tmem + lane_base + kChunkColO + 128 * w;
         const int i = w * per + r / A.G;         // token of the tile
         uint32_t s_count = 0, o_count = 0;
-        if (tid == 0) A.records[blockIdx.x].first = -1;
         while (next(d)) {
             // what decides the loop's course is the same in all lanes (2048 tokens on 32768 930 us without the compiler knowing it, 904 with)
             const int j0 = uniform(d.j0), end = uniform(w ? d.end[1] : d.end[0]), fewest = uniform(w ? d.fewest[1] : d.fewest[0]);

@@ -43,10 +43,11 @@ struct __align__(1024) FewSmem {
     PagedRun<kFewShift, kFewItem> run;
     int32_t bad[kStages];                       // the tile's first key that lies on an entry that is no page; kNoKey: all its entries are pages
     volatile uint32_t failed;
+    uint32_t* expired;                          // where the call's status has this block
 };
 
 // Bounded waits.
-__device__ __forceinline__ bool paged_poll(uint64_t* bar, uint32_t parity, volatile uint32_t* failed)
+__device__ __forceinline__ bool paged_poll(uint64_t* bar, uint32_t parity, volatile uint32_t* failed, uint32_t* expired)
 {
 #pragma unroll 1
     for (int i = 0; i < 20000; ++i) {           // a second at most
@@ -54,12 +55,13 @@ __device__ __forceinline__ bool paged_poll(uint64_t* bar, uint32_t parity, volat
         if (ptx::mbar_try_wait_suspend(bar, parity, 50000u)) return true;
     }
     *failed = 1u;
+    *expired = 1u;
     return false;
 }
 template <typename Smem>
 __device__ __forceinline__ bool paged_wait(uint64_t* bar, uint32_t parity, Smem* sm)
 {
-    return ptx::mbar_try_wait(bar, parity) || paged_poll(bar, parity, &sm->failed);
+    return ptx::mbar_try_wait(bar, parity) || paged_poll(bar, parity, &sm->failed, sm->expired);
 }
 
 // The same for a warp, whose lanes leave the wait together: what follows needs all of them (ldmatrix, mma, ballots).
@@ -134,6 +136,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
         sm->failed = 0u;
+        sm->expired = A.expired + blockIdx.x;
         for (int i = 0; i < kStages; ++i) {
             ptx::mbar_init(&sm->full[i], 1);
             ptx::mbar_init(&sm->empty[i], kFewWarps / 2);
@@ -149,6 +152,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
     }
     ptx::grid_wait();
     ptx::grid_launch_next();
+    if (tid == kFewWarps * 32) paged_begin_status(A);
     paged_find_run<kFewThreads, kFewShift, kFewItem>(A, sm->scratch, &sm->run);      // barriers of the block
     PagedWalk<kFewShift, kFewItem, PagedReader<kFewShift, kFewItem>> walk(PagedReader<kFewShift, kFewItem>{A}, A.n_seqs, A.Hkv, sm->run);
     PagedSegment<kFewShift, kFewItem> g;
@@ -210,7 +214,6 @@ paged_few_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
     // the lane's row of a matrix of K (8 keys x 16 bytes) and of V; both have the swizzle of lane & 7
     const uint32_t k_at = ((sub >> 3) + (lane >> 4)) * 2048 + (lane & 7) * 128, v_at = ((sub >> 3) + ((lane >> 3) & 1)) * 2048 + (lane & 7) * 128;
     uint32_t tile = 0, seg = 0;
-    if (tid == 0) A.records[blockIdx.x].first = -1;
     while (walk.next(g)) {
         const uint32_t qb = seg & 1u;
         uint32_t qa[8][4];

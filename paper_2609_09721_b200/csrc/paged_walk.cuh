@@ -1,6 +1,7 @@
 // How the kernels of the paged attention share a step's work (paged_units.h), on the device.
 #pragma once
 
+#include "efq_internal.cuh"
 #include "paged.cuh"
 #include "paged_units.h"
 #include "sm100_ptx.cuh"
@@ -29,6 +30,8 @@ struct PagedArgs {
     float* part_o;
     float2* part_ml;                    // maximum (of the scores times scale_log2) and sum
     PagedRecord* records;
+    uint32_t* header;                   // of the workspace: kPagedStatus, the number of CTAs
+    uint32_t* expired;                  // of every CTA: a bounded wait has run out there
     int32_t inject_skip_loads;
 };
 
@@ -110,6 +113,14 @@ __device__ __noinline__ void paged_find_run(const PagedArgs& A, uint32_t* scratc
     for (int i = tid; i < tiles; i += kThreads)
         if (paged_begin_tile(i, shares, c, run)) break;
     __syncthreads();
+}
+
+// What a CTA leaves before its waits: called by one thread, and a barrier of the block has to follow.
+__device__ __forceinline__ void paged_begin_status(const PagedArgs& A)
+{
+    A.expired[blockIdx.x] = 0u;
+    A.records[blockIdx.x].first = -1;
+    if (blockIdx.x == 0) *reinterpret_cast<uint2*>(A.header) = make_uint2(kPagedStatus, gridDim.x);
 }
 
 // Keys that token i of the segment's tile sees

@@ -266,3 +266,28 @@ def test_scales_that_are_infinite_in_units_of_log2_are_refused():
         assert _attention(_rows(), _cache(), scale=scale) == INVALID, scale
     for scale in (2.3e38, 1e-45, -1.0, float("-inf")):
         assert _attention(_rows(), _cache(), scale=scale, total=0) == OK, scale
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,seqs", [(1, 2), (6, 2), (40, 2), (1, 300), (7, 90)])
+def test_the_status_of_a_call_is_in_its_workspace(n, seqs):
+    """0 after a call, whatever stood there; the time-out after one whose waits expired; 0 again after the next."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    q = torch.randn(seqs * n, 8, 128, generator=g, device="cuda").bfloat16()
+    cache = torch.randn(40, 2, 16, 128, generator=g, device="cuda").bfloat16()
+    table = torch.randint(0, 40, (seqs, 20), generator=g, dtype=torch.int32, device="cuda")
+    cu = torch.arange(0, seqs * n + 1, n, dtype=torch.int32, device="cuda")
+    lens = torch.tensor([n + (i * 37 + 250) % 260 for i in range(seqs)], dtype=torch.int32, device="cuda")
+    nbytes = binding.efq_paged_attention_workspace_bytes(8, 2, n)
+    guard = torch.full((nbytes + 4096,), 255, dtype=torch.uint8, device="cuda")
+    ws, o, side = guard[:nbytes], torch.empty_like(q), torch.cuda.Stream()
+    args = (q, cache, cache, table, cu, lens, n)
+    for _ in range(2):
+        binding.efq_paged_attention_fwd(*args, o=o, workspace=ws)
+        assert binding.efq_poll_status(ws) == OK
+        binding.efq_paged_attention_fwd_inject_timeout(*args, o, ws)
+        assert binding.efq_poll_status(ws) == binding.STATUS_NAMES.index("EFQ_ERR_DEVICE_TIMEOUT")
+    torch.cuda.synchronize()
+    binding.efq_paged_attention_fwd(*args, o=o, workspace=ws, stream=side)
+    assert binding.efq_poll_status(ws, side) == OK and torch.isfinite(o).all()
+    assert (guard[nbytes:] == 255).all()
