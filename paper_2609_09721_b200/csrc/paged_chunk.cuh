@@ -512,8 +512,9 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
                 for (int q = 0; q < 8; ++q) top[q] = max3(top[q], s[120 + q], top[q]);
                 const float mx = max3(max3(top[0], top[1], top[2]), max3(top[3], top[4], top[5]), max3(top[6], top[7], top[7])) * A.scale_log2;
                 const float reference = paged_reference(mx, kChunkRaise<T>);
-                const bool grew = !(reference <= __fadd_rd(m, kSlack<T>));        // also a NaN; a step of m may be more than the slack
-                const bool far = fabsf(mx) > kFar && fabsf(mx) < INFINITY;
+                // rows that no query has hold anything, and their output is not stored: nothing is done for what they hold
+                const bool grew = mine && !(reference <= __fadd_rd(m, kSlack<T>));        // also a NaN; a step of m may be more than the slack
+                const bool far = mine && fabsf(mx) > kFar && fabsf(mx) < INFINITY;
                 float scale = A.scale_log2;
                 if (__any_sync(0xffffffffu, grew || far)) {
                     if (__any_sync(0xffffffffu, far)) {

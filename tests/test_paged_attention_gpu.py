@@ -427,3 +427,29 @@ def test_a_maximum_that_grows_by_little_far_from_zero(grows, max_q):
     near = ((v[0] + w * v[300]) / (1 + w))[None].cuda()          # the steps of 2 are exact here: probabilities and the output are rounded once
     bound = 2.0 ** -11 * ((v[0].abs() + w * v[300].abs()) / (1 + w)).cuda() * 2.1 + 700 * 2.0 ** -32 * 4
     assert float(((o.double() - near).abs() - bound).max()) <= 0.0
+
+
+def _ms(call):
+    a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    a.record()
+    call()
+    b.record()
+    b.synchronize()
+    return a.elapsed_time(b)
+
+
+@pytest.mark.parametrize("n,Hq,Hkv", [(33, 32, 32), (5, 256, 32), (100, 32, 32)])
+def test_rows_that_no_query_has_do_not_matter_to_the_time(n, Hq, Hkv):
+    """Rows behind the last sequence lie in its query tile too.  Nothing that they hold may be a reason to rescale the output, as a maximum that is
+    NaN is at every tile of keys: both kinds of rows take the same time, but for the clock (5 %)."""
+    p = Paged([(n, 20000)], Hq, Hkv, 128, seed=23, tail=256)
+    rows = {"zero": p.d_q.clone(), "nan": p.d_q.clone()}
+    rows["zero"][n:] = 0.0
+    rows["nan"][n:] = math.nan
+    workspace = torch.empty(binding.efq_paged_attention_workspace_bytes(Hq, Hkv, 1000), dtype=torch.uint8, device="cuda")
+    o = torch.empty_like(p.d_q)
+    times = {x: 1e9 for x in rows}
+    for _ in range(40):
+        for x, q in rows.items():
+            times[x] = min(times[x], _ms(lambda: binding.efq_paged_attention_fwd(q, p.d_k_cache, p.d_v_cache, *p.tables, 1000, o=o, workspace=workspace)))
+    assert times["nan"] <= 1.05 * times["zero"], times
