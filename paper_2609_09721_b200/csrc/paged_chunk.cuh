@@ -53,6 +53,7 @@ struct __align__(16) ChunkSegment {
 constexpr int kChunkSegments = 4;
 
 struct __align__(1024) ChunkSmem {
+    static constexpr bool kExpired = false;                    // an expired wait is told at the end of the block
     uint8_t q[2][2][kChunkPart];                               // half, channels 0-63 and 64-127; 128-byte swizzle
     uint8_t kv[kChunkSlots][2 * kChunkPart];                   // [8 tokens][channels 0-63, 64-127][token]
     uint64_t full[kChunkSlots], empty[kChunkSlots], q_full, q_empty, s_full[2], p_ready[2], p_rest[2], o_full[2], v_tail, v_clean, drained[2];
@@ -62,7 +63,6 @@ struct __align__(1024) ChunkSmem {
     PagedRun<kChunkShift, kChunkItem> run;
     uint32_t tmem_base;
     volatile uint32_t failed;
-    uint32_t* expired;                          // where the call's status has this block
 };
 
 // Registers of a softmax thread, which holds a row of scores, and of the others: together what the block is launched with, 384 x 168.  208 and 88: 2048
@@ -170,10 +170,7 @@ __device__ __forceinline__ bool chunk_segment_wait(uint64_t* bar, uint32_t parit
     bool there = ptx::mbar_try_wait(bar, parity);
 #pragma unroll 1
     for (int i = 0; !there && i < 40000; ++i) there = ptx::mbar_try_wait_suspend(bar, parity, 50000u);
-    if (!there) {
-        sm->failed = 1u;
-        *sm->expired = 1u;
-    }
+    if (!there) sm->failed = 1u;
     return __all_sync(0xffffffffu, there) != 0;
 }
 
@@ -187,7 +184,6 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
     const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
     if (tid == 0) {
         sm->failed = 0u;
-        sm->expired = A.expired + blockIdx.x;
         for (int i = 0; i < kChunkSlots; ++i) {
             ptx::mbar_init(&sm->full[i], 1);
             ptx::mbar_init(&sm->empty[i], 2);
@@ -510,11 +506,11 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
                     for (int q = 0; q < 8; ++q) top[q] = max3(top[q], s[c + q], s[c + 8 + q]);
 #pragma unroll
                 for (int q = 0; q < 8; ++q) top[q] = max3(top[q], s[120 + q], top[q]);
-                const float mx = max3(max3(top[0], top[1], top[2]), max3(top[3], top[4], top[5]), max3(top[6], top[7], top[7])) * A.scale_log2;
+                float mx = max3(max3(top[0], top[1], top[2]), max3(top[3], top[4], top[5]), max3(top[6], top[7], top[7])) * A.scale_log2;
+                mx = mine ? mx : -INFINITY;          // rows that no query has hold anything, and their output is not stored: nothing is done for what they hold
                 const float reference = paged_reference(mx, kChunkRaise<T>);
-                // rows that no query has hold anything, and their output is not stored: nothing is done for what they hold
-                const bool grew = mine && !(reference <= __fadd_rd(m, kSlack<T>));        // also a NaN; a step of m may be more than the slack
-                const bool far = mine && fabsf(mx) > kFar && fabsf(mx) < INFINITY;
+                const bool grew = !(reference <= __fadd_rd(m, kSlack<T>));        // also a NaN; a step of m may be more than the slack
+                const bool far = fabsf(mx) > kFar && fabsf(mx) < INFINITY;
                 float scale = A.scale_log2;
                 if (__any_sync(0xffffffffu, grew || far)) {
                     if (__any_sync(0xffffffffu, far)) {
@@ -616,6 +612,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant
     }
     ptx::tc_fence_before_sync();
     __syncthreads();
+    if (tid == 0 && sm->failed != 0u) A.expired[blockIdx.x] = 1u;
     if (warp == 8) ptx::tmem_dealloc(tmem, 512);
 }
 

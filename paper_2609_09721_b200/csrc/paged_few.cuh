@@ -28,6 +28,7 @@ template <typename T> constexpr float kFewRaise = kNarrowExponent<T> ? 15.0f : 0
 
 template <int kRows>
 struct __align__(1024) FewSmem {
+    static constexpr bool kExpired = true;      // an expired wait is told at once (at the end of the block: 512 tokens on 100 keys each 1 us more)
     // Even, so that a stage's tiles all belong to one group of four warps: a group that skipped every other phase of a barrier could take the
     // phase before last for the last one, since loads may land in another order than they were issued in.
     static constexpr int kStages = 4;
@@ -55,13 +56,15 @@ __device__ __forceinline__ bool paged_poll(uint64_t* bar, uint32_t parity, volat
         if (ptx::mbar_try_wait_suspend(bar, parity, 50000u)) return true;
     }
     *failed = 1u;
-    *expired = 1u;
+    if (expired != nullptr) *expired = 1u;
     return false;
 }
 template <typename Smem>
 __device__ __forceinline__ bool paged_wait(uint64_t* bar, uint32_t parity, Smem* sm)
 {
-    return ptx::mbar_try_wait(bar, parity) || paged_poll(bar, parity, &sm->failed, sm->expired);
+    if (ptx::mbar_try_wait(bar, parity)) return true;
+    if constexpr (Smem::kExpired) return paged_poll(bar, parity, &sm->failed, sm->expired);
+    else return paged_poll(bar, parity, &sm->failed, nullptr);
 }
 
 // The same for a warp, whose lanes leave the wait together: what follows needs all of them (ldmatrix, mma, ballots).
