@@ -152,7 +152,17 @@ bool cache_of(Checked& c, PyObject* const* a, efq_paged_t& p)
 #define UNLOCKED(call) \
     efq_status_t st; \
     Py_BEGIN_ALLOW_THREADS st = call; \
-    Py_END_ALLOW_THREADS return PyLong_FromLong(st);
+    Py_END_ALLOW_THREADS
+
+// What a call has written counts as changed in place, so that autograd refuses a backward pass that has kept what stood there before.  Tensors of the
+// inference mode have no count.
+PyObject* wrote(efq_status_t st, std::initializer_list<PyObject*> outputs)
+{
+    for (PyObject* o : outputs)
+        if (st == EFQ_OK && o != Py_None)
+            if (const at::Tensor& t = THPVariable_Unpack(o); !t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+    return PyLong_FromLong(st);
+}
 
 // q, k, positions, rotary, inverse, q_out, k_out, device, stream
 PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n)
@@ -182,6 +192,7 @@ PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n)
     const int64_t axis = p->stride(0), batch = batched ? p->stride(1) : 0;
     UNLOCKED(rotary_fn(has_q ? &q : nullptr, has_k ? &k : nullptr, static_cast<const int32_t*>(p->const_data_ptr()), axis, batch, static_cast<int>(B), S, kD, c.dtype(),
                        description, inverse, stream))
+    return wrote(st, {has_q ? a[5] : Py_None, has_k ? a[6] : Py_None});
 }
 
 // k, v, cache, rotary, positions, q, q_out, device, stream
@@ -212,6 +223,7 @@ PyObject* paged_append(PyObject*, PyObject* const* a, Py_ssize_t n)
     if (c.wrong != nullptr) return refused(c);
     UNLOCKED(append_fn(&kr, &vr, q != nullptr ? &qr : nullptr, total, p != nullptr ? static_cast<const int32_t*>(p->const_data_ptr()) : nullptr,
                        p != nullptr ? p->stride(0) : 0, &cache, kD, c.dtype(), description, stream))
+    return wrote(st, {a[2], a[3], q != nullptr ? b[3] : Py_None});
 }
 
 // q, cache, max_seqlen_q, causal, scale, o, lse, workspace, device, stream
@@ -242,6 +254,7 @@ PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n)
     if (c.wrong != nullptr) return refused(c);
     UNLOCKED(attention_fn(&qr, lse != nullptr ? static_cast<float*>(lse->data_ptr()) : nullptr, q->size(0), static_cast<int>(max_q), &cache, kD, c.dtype(),
                           causal != 0, scale, ws->data_ptr(), static_cast<size_t>(ws->numel()), stream))
+    return wrote(st, {b[3], b[4]});
 }
 
 template <PyObject* (*f)(PyObject*, PyObject* const*, Py_ssize_t)>

@@ -257,3 +257,58 @@ def test_nothing_to_do():
     binding.efq_paged_append(k, k, p.d_k_cache, p.d_v_cache, p.d_table[:0], zero, none, r, None, p.d_q, q)
     binding.efq_paged_append(k, k, p.d_k_cache, p.d_v_cache, p.d_table, torch.zeros(2, dtype=torch.int32, device="cuda"), p.d_seq_lens, r, None, p.d_q, q)
     assert (q == 7.0).all() and torch.equal(before.view(torch.int16), p.d_v_cache.view(torch.int16))
+
+
+def _step():
+    p = Paged([(5, 50), (1, 300)], 4, 2, 16, seed=31)
+    k, v = (torch.randn(6, 2, D, device="cuda").bfloat16() for _ in range(2))
+    return p, k, v, _rotary((64,), False, False)
+
+
+def test_what_is_written_counts_as_changed():
+    """A tensor's version grows with every call that writes it, and with none that reads it, so that autograd notices that a value it kept is gone."""
+    p, k, v, r = _step()
+    q_out, lse, o = torch.empty_like(p.d_q), torch.zeros(p.total, 4, device="cuda"), torch.empty_like(p.d_q)
+    x, y = p.d_q.transpose(0, 1)[None], k.transpose(0, 1)[None]
+    pos = _positions(1, 6, 0)
+    read = [k, v, p.d_q, *p.tables, pos, r.inv_freq]
+    before = [t._version for t in read]
+
+    def grows(call, *written):
+        old = [t._version for t in written]
+        call()
+        assert all(t._version > a for t, a in zip(written, old)) and [t._version for t in read] == before
+
+    grows(lambda: binding.efq_paged_append(k, v, p.d_k_cache, p.d_v_cache, *p.tables, r, None, p.d_q, q_out), p.d_k_cache, p.d_v_cache, q_out)
+    grows(lambda: binding.efq_paged_append(k, v, p.d_k_cache, p.d_v_cache, *p.tables), p.d_k_cache, p.d_v_cache)
+    grows(lambda: binding.efq_paged_attention_fwd(q_out, p.d_k_cache, p.d_v_cache, *p.tables, 5, o=o, lse=lse), o, lse)
+    grows(lambda: binding.efq_paged_attention_fwd(q_out, p.d_k_cache, p.d_v_cache, *p.tables, 5, o=o), o)
+    a, b = torch.empty_like(x), torch.empty_like(y)
+    grows(lambda: binding.efq_rotary(x, y, pos, r, q_out=a, k_out=b), a, b)
+    grows(lambda: binding.efq_rotary(a, None, pos, r, q_out=a), a)
+    w = torch.randn(D, 3, device="cuda", dtype=torch.bfloat16, requires_grad=True)
+    kept = p.d_v_cache.clone()[0, 0]
+    table = torch.zeros_like(p.d_table)
+    cache = kept[None, None].clone()
+    loss = (cache[0, 0] @ w).sum()                                # keeps the cache for w's gradient
+    lens, cu = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([1], [0, 1]))
+    binding.efq_paged_append(k[:1, :1], v[:1, :1], cache.clone(), cache, table[:1], cu, lens)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+
+
+def test_tensors_of_the_inference_mode():
+    """They have no version; what they get is the same, in the mode and outside."""
+    p, k, v, r = _step()
+    q_out = binding.efq_paged_append(k, v, p.d_k_cache, p.d_v_cache, *p.tables, r, None, p.d_q)
+    want = binding.efq_paged_attention_fwd(q_out, p.d_k_cache, p.d_v_cache, *p.tables, 5)
+    with torch.inference_mode():
+        kc, vc, q2 = torch.empty_like(p.d_k_cache), torch.empty_like(p.d_v_cache), torch.empty_like(q_out)
+        kc.copy_(p.d_k_cache)
+        vc.copy_(p.d_v_cache)
+        binding.efq_paged_append(k, v, kc, vc, *p.tables, r, None, p.d_q, q2)
+        assert torch.equal(binding.efq_paged_attention_fwd(q2, kc, vc, *p.tables, 5), want)
+    o = torch.empty_like(want)
+    binding.efq_paged_append(k, v, kc, vc, *p.tables, r, None, p.d_q, q2)
+    assert torch.equal(binding.efq_paged_attention_fwd(q2, kc, vc, *p.tables, 5, o=o), want)
+    assert torch.equal(binding.efq_rotary(q2.transpose(0, 1)[None], None, _positions(1, 6, 0), r, q_out=q2.transpose(0, 1)[None])[0][0].transpose(0, 1), q2)
