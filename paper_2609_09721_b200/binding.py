@@ -70,6 +70,7 @@ class EfqError(RuntimeError):
 _lib = None
 _fast = None
 _tensors = None
+_grad_enabled = torch.is_grad_enabled
 _raw_stream, _raw_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice    # a tenth of torch.cuda.current_stream()
 
 
@@ -493,14 +494,19 @@ class Rotary:
         return cls(torch.tensor([float(theta) ** -x for x in steps], dtype=torch.float64, device=device or "cuda"), sections, interleaved)
 
 
+def _stream_object(stream):
+    """A stream that a call was given, as torch takes it; None, which stays None, is the current one."""
+    if stream is None or hasattr(stream, "cuda_stream"):
+        return stream
+    return torch.cuda.ExternalStream(int(stream)) if int(stream) != 0 else torch.cuda.default_stream()
+
+
 def _new(shape, dtype, device, stream):
     """A tensor that belongs to the stream of the call: memory that the current stream may still be using, or may be given next, is no
     place for what another one writes."""
     if stream is None:
         return torch.empty(shape, dtype=dtype, device=device)
-    if not hasattr(stream, "cuda_stream"):
-        stream = torch.cuda.ExternalStream(int(stream)) if int(stream) != 0 else torch.cuda.default_stream()
-    with torch.cuda.stream(stream):
+    with torch.cuda.stream(_stream_object(stream)):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
@@ -508,10 +514,43 @@ def _out(x, out, stream):
     return _new(x.shape, x.dtype, x.device, stream) if out is None and x is not None else out
 
 
+class _Turned(torch.autograd.Function):
+    """efq_rotary into new tensors.  It is linear: the gradients are the outputs' gradients turned the other way."""
+
+    @staticmethod
+    def forward(ctx, q, k, positions, rotary, inverse):
+        ctx.save_for_backward(positions)
+        ctx.rotary, ctx.inverse = rotary, inverse
+        ctx.set_materialize_grads(False)
+        out = _rotary(q, k, positions, rotary, inverse, None, None, None)
+        ctx.mark_non_differentiable(*(y for y, needed in zip(out, ctx.needs_input_grad) if y is not None and not needed))
+        return out
+
+    @staticmethod
+    def backward(ctx, *grads):
+        positions, = ctx.saved_tensors
+        # as the kernel reads rows: a sum's gradient, for one, is a number without strides
+        dq, dk = (g if g is None or (g.stride(-1) == 1 and g.data_ptr() % 16 == 0 and not any(n % 8 for n in g.stride()[:-1])) else g.contiguous() for g in grads)
+        if dq is not None or dk is not None:
+            dq, dk = efq_rotary(dq, dk, positions, ctx.rotary, not ctx.inverse)
+        return dq, dk, None, None, None
+
+
 def efq_rotary(q, k, positions, rotary: Rotary, inverse: bool = False, q_out=None, k_out=None, stream=None):
     """Rotary positions turned into q [B, Hq, S, 128] and k [B, Hkv, S, 128] (bf16 or fp16, any strides; either may be None) in one
     launch.  positions: int32 [axes, S], or [axes, B, S].  q_out and k_out: the outputs (q and k themselves: in place); new tensors are
-    contiguous, as the forwards take them.  inverse: turned back, which is the gradient.  Returns (q_out, k_out)."""
+    contiguous, as the forwards take them.  inverse: turned back, which is the gradient.  Returns (q_out, k_out).
+
+    Where q or k requires a gradient, the new outputs carry it on; outputs that are given cannot, and are refused."""
+    if _grad_enabled() and (q is not None and q.requires_grad or k is not None and k.requires_grad
+                            or q_out is not None and q_out.requires_grad or k_out is not None and k_out.requires_grad):
+        assert q_out is None and k_out is None, "efq_rotary: q_out and k_out carry no gradient; leave them out, or call it under torch.no_grad()"
+        with torch.cuda.stream(_stream_object(stream)):          # that of the backward pass, too
+            return _Turned.apply(q, k, positions, rotary, bool(inverse))
+    return _rotary(q, k, positions, rotary, inverse, q_out, k_out, stream)
+
+
+def _rotary(q, k, positions, rotary, inverse, q_out, k_out, stream):
     q_out, k_out = _out(q, q_out, stream), _out(k, k_out, stream)
     st = (_tensors or _tensorcall()).rotary(q, k, positions, rotary.address_on(_raw_device()), 1 if inverse else 0, q_out, k_out, _raw_device(), _stream(stream))
     if st:
@@ -524,7 +563,7 @@ def efq_paged_append(k, v, k_cache, v_cache, page_table, cu_seqlens, seq_lens, r
     """Writes the new keys (rotated) and values of a step, [total, Hkv, 128], into the paged cache [pages, Hkv, page_size, 128] and
     rotates q [total, Hq, 128] beside them.  cu_seqlens [n_seqs + 1], seq_lens [n_seqs], page_table [n_seqs, max_pages]: int32 CUDA tensors;
     seq_lens counts the new tokens too.  positions: int32 [axes, total], None: a token's index in its sequence.  Returns q_out, or None
-    without q."""
+    without q.  For serving: nothing that it writes has a gradient."""
     q_out = _out(q, q_out, stream)
     device = _raw_device()
     st = (_tensors or _tensorcall()).paged_append(k, v, k_cache, v_cache, page_table, cu_seqlens, seq_lens, None if rotary is None else rotary.address_on(device),
@@ -546,7 +585,8 @@ def _paged_workspace(q, k_cache, max_seqlen_q, stream):
 def efq_paged_attention_fwd(q, k_cache, v_cache, page_table, cu_seqlens, seq_lens, max_seqlen_q: int, causal: bool = True,
                             softmax_scale: float = 0.0, o=None, lse=None, workspace=None, stream=None):
     """Softmax attention of a step's new tokens q [total, Hq, 128] over a paged cache [pages, Hkv, page_size, 128] (tables as for
-    efq_paged_append); max_seqlen_q: the most new tokens of any sequence.  lse: optional fp32 [total, Hq] output.  Returns o, of q's type."""
+    efq_paged_append); max_seqlen_q: the most new tokens of any sequence.  lse: optional fp32 [total, Hq] output.  Returns o, of q's type,
+    which has no gradient, as the forwards' outputs."""
     o = _out(q, o, stream)
     if workspace is None:
         workspace = _paged_workspace(q, k_cache, max_seqlen_q, stream)

@@ -312,3 +312,103 @@ def test_tensors_of_the_inference_mode():
     binding.efq_paged_append(k, v, kc, vc, *p.tables, r, None, p.d_q, q2)
     assert torch.equal(binding.efq_paged_attention_fwd(q2, kc, vc, *p.tables, 5, o=o), want)
     assert torch.equal(binding.efq_rotary(q2.transpose(0, 1)[None], None, _positions(1, 6, 0), r, q_out=q2.transpose(0, 1)[None])[0][0].transpose(0, 1), q2)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("sections,interleaved,inverse", [((64,), False, False), ((22, 21, 21), True, False), ((20, 12), False, True), ((5, 3), True, True)])
+def test_gradients(dtype, sections, interleaved, inverse):
+    """Through autograd: of both tensors, of one of them, of a projection that both are views of, and of a sum; against the formula in 64 bits."""
+    B, S, Hq, Hkv = 2, 37, 5, 3
+    g = torch.Generator(device="cuda").manual_seed(32)
+    r, pos = _rotary(sections, interleaved, False), _positions(len(sections), S, 700)
+    q, k, wq, wk = (torch.randn(B, H, S, D, generator=g, device="cuda").to(dtype) for H in (Hq, Hkv, Hq, Hkv))
+
+    def want(w):
+        return rotate(w, pos, r.inv_freq, sections, interleaved, not inverse), rotate_slack(w, dtype, sections, interleaved)
+
+    plain = binding.efq_rotary(q, k, pos, r, inverse)
+    q.requires_grad_()
+    k.requires_grad_()
+    y = binding.efq_rotary(q, k, pos, r, inverse)
+    assert all(a.requires_grad and torch.equal(a, b) for a, b in zip(y, plain))
+    dq, dk = torch.autograd.grad(y, (q, k), (wq, wk))
+    _near(dq, *want(wq))
+    _near(dk, *want(wk))
+    assert all(torch.equal(a, b) for a, b in zip((dq, dk), binding.efq_rotary(wq, wk, pos, r, not inverse)))
+    for a, b, w in ((q, None, wq), (None, k, wk)):               # one tensor alone
+        y = [x for x in binding.efq_rotary(a, b, pos, r, inverse) if x is not None]
+        _near(torch.autograd.grad(y[0], a if b is None else b, w)[0], *want(w))
+    yq, yk = binding.efq_rotary(q, k.detach(), pos, r, inverse)   # one of the two
+    assert yq.requires_grad and not yk.requires_grad
+    assert torch.equal(torch.autograd.grad(yq, q, wq)[0], dq)
+    yq, yk = binding.efq_rotary(q, k, pos, r, inverse)            # one output is not used
+    got = torch.autograd.grad(yk, (q, k), wk, allow_unused=True)
+    assert got[0] is None and torch.equal(got[1], dk)
+    ones = torch.ones(B, Hq, S, D, dtype=dtype, device="cuda")
+    _near(torch.autograd.grad(binding.efq_rotary(q, None, pos, r, inverse)[0].sum(), q)[0], *want(ones))
+    _near(torch.autograd.grad(binding.efq_rotary(q, None, pos, r, inverse)[0].transpose(2, 3).contiguous(), q, wq.transpose(2, 3).contiguous())[0], *want(wq))
+    x = torch.randn(B, S, Hq + 2 * Hkv, D, generator=g, device="cuda").to(dtype).requires_grad_()
+    yq, yk = binding.efq_rotary(x[:, :, :Hq].transpose(1, 2), x[:, :, Hq:Hq + Hkv].transpose(1, 2), pos, r, inverse)
+    torch.autograd.backward((yq, yk), (wq, wk))
+    assert torch.equal(x.grad[:, :, :Hq].transpose(1, 2), dq) and torch.equal(x.grad[:, :, Hq:Hq + Hkv].transpose(1, 2), dk) and (x.grad[:, :, Hq + Hkv:] == 0).all()
+
+
+def test_gradients_of_gradients_and_of_changed_positions():
+    g = torch.Generator(device="cuda").manual_seed(33)
+    r, pos = _rotary((64,), False, False), _positions(1, 9, 50)
+    q, w, u = (torch.randn(1, 2, 9, D, generator=g, device="cuda").bfloat16() for _ in range(3))
+    q.requires_grad_()
+    w.requires_grad_()
+    dq, = torch.autograd.grad(binding.efq_rotary(q, None, pos, r)[0], q, w, create_graph=True)
+    ddw, = torch.autograd.grad(dq, w, u)                          # dq is w turned back, so u is turned on
+    assert torch.equal(ddw, binding.efq_rotary(u, None, pos, r)[0])
+    y, _ = binding.efq_rotary(q, None, pos, r)
+    pos.add_(1)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward(w.detach())
+
+
+def test_where_there_is_no_gradient():
+    """Outputs that are given: refused where a gradient would be lost.  Without gradients all is as before."""
+    r, pos = _rotary((64,), False, False), _positions(1, 9, 50)
+    q = torch.randn(1, 2, 9, D, device="cuda").bfloat16().requires_grad_()
+    k = q.detach().clone()
+    want = binding.efq_rotary(k, None, pos, r)[0]
+    for args in (dict(q_out=torch.empty_like(k)), dict(q_out=q), dict(q_out=k)):
+        with pytest.raises(AssertionError, match="no_grad"):
+            binding.efq_rotary(q, None, pos, r, **args)
+    with pytest.raises(AssertionError, match="no_grad"):
+        binding.efq_rotary(k, None, pos, r, q_out=q)
+    with pytest.raises(AssertionError, match="no_grad"):
+        binding.efq_rotary(k, q, pos, r, k_out=torch.empty_like(k))
+    with torch.no_grad():
+        y, _ = binding.efq_rotary(q, None, pos, r)
+        assert not y.requires_grad and torch.equal(y, want)
+        assert torch.equal(binding.efq_rotary(q, None, pos, r, q_out=torch.empty_like(k))[0], want)
+    assert not binding.efq_rotary(k, k, pos, r)[1].requires_grad
+    for bad in ((q.float(), None, pos), (q, None, pos[:, :4]), (q, k[:, :, :4], pos)):
+        with pytest.raises(AssertionError):
+            binding.efq_rotary(*bad, r)
+
+
+def test_gradients_on_a_side_stream_and_in_a_graph():
+    g = torch.Generator(device="cuda").manual_seed(34)
+    r, pos = _rotary((64,), False, False), _positions(1, 4000, 50)
+    q, w = (torch.randn(1, 8, 4000, D, generator=g, device="cuda").bfloat16() for _ in range(2))
+    want = binding.efq_rotary(w, None, pos, r, inverse=True)[0]
+    q.requires_grad_()
+    s = torch.cuda.Stream()
+    for stream in (s, s.cuda_stream):
+        s.wait_stream(torch.cuda.current_stream())
+        y, _ = binding.efq_rotary(q, None, pos, r, stream=stream)
+        torch.cuda.current_stream().wait_stream(s)
+        dq, = torch.autograd.grad(y, q, w)
+        assert torch.equal(dq, want)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y, _ = binding.efq_rotary(q, None, pos, r)
+        dq, = torch.autograd.grad(y, q, w)
+    w.copy_(w.flip(2))
+    graph.replay()
+    assert torch.equal(dq, binding.efq_rotary(w, None, pos, r, inverse=True)[0])
