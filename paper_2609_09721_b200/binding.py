@@ -171,10 +171,15 @@ def _tensorcall():
     global _tensors
     if _tensors is None:
         L = lib()
+        from . import build
         try:
             from . import efq_tensorcall
         except ImportError as e:
-            raise RuntimeError("efq_tensorcall.so is missing: build it with `python -m paper_2609_09721_b200.build`") from e
+            what = "cannot be loaded (it is compiled against one torch and Python)" if os.path.exists(build.TENSORCALL) else "is missing"
+            raise RuntimeError(f"efq_tensorcall.so {what}: build it with `python -m paper_2609_09721_b200.build`") from e
+        if getattr(efq_tensorcall, "built_for", "another torch") != build.target():      # tensors would be misread
+            raise RuntimeError(f"efq_tensorcall.so was built for {getattr(efq_tensorcall, 'built_for', 'another torch')}, this is {build.target()}: "
+                               "build it with `python -m paper_2609_09721_b200.build`")
         address = lambda f: C.cast(f, C.c_void_p).value
         efq_tensorcall.set_functions(address(L.efq_rotary), address(L.efq_paged_append), address(L.efq_paged_attention_fwd))
         _tensors = efq_tensorcall

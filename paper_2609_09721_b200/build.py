@@ -16,6 +16,7 @@ FASTCALL_SRC = os.path.join(CSRC, "fastcall.c")
 FASTCALL = os.path.join(_HERE, "efq_fastcall.so")
 TENSORCALL_SRC = os.path.join(CSRC, "tensorcall.cpp")
 TENSORCALL = os.path.join(_HERE, "efq_tensorcall.so")
+BUILT_FOR = os.path.join(_HERE, "build", "efq_tensorcall.built_for")
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo",
@@ -27,9 +28,22 @@ def sources():
     return sorted(glob.glob(os.path.join(CSRC, "*.cu")))
 
 
+def target() -> str:
+    """What efq_tensorcall.so, which is compiled against torch's C++ headers, is good for."""
+    import torch
+    return f"torch {torch.__version__}, C++ ABI {int(torch._C._GLIBCXX_USE_CXX11_ABI)}, Python {sysconfig.get_config_var('EXT_SUFFIX')}"
+
+
+def _built_for() -> str:
+    if not os.path.exists(BUILT_FOR):
+        return ""
+    with open(BUILT_FOR) as f:
+        return f.read()
+
+
 def _stale() -> bool:
     built = (LIB, FASTCALL, TENSORCALL)
-    if not all(os.path.exists(f) for f in built):
+    if not all(os.path.exists(f) for f in built) or _built_for() != target():
         return True
     t = min(os.path.getmtime(f) for f in built)
     deps = sources() + [FASTCALL_SRC, TENSORCALL_SRC] + glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(ROOT, "include", "*.h"))
@@ -40,7 +54,7 @@ def _start_tensorcall(out: str):
     import torch
     torch_dir = os.path.dirname(torch.__file__)
     return subprocess.Popen([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-Wall", "-shared", "-fPIC",
-                             f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", sysconfig.get_paths()["include"],
+                             f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f'-DEFQ_BUILT_FOR="{target()}"', "-I", sysconfig.get_paths()["include"],
                              "-I", os.path.join(ROOT, "include"), "-isystem", os.path.join(torch_dir, "include"), TENSORCALL_SRC, "-o", out,
                              "-L", os.path.join(torch_dir, "lib"), "-lc10", "-ltorch_cpu", "-ltorch_python"],
                             stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
@@ -78,6 +92,8 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if tensorcall.returncode != 0:
         raise RuntimeError(f"g++ failed on {TENSORCALL_SRC}")
     os.replace(tensorcall_tmp, TENSORCALL)
+    with open(BUILT_FOR, "w") as f:
+        f.write(target())
     return LIB
 
 

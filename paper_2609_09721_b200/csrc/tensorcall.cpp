@@ -281,4 +281,13 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "efq_tensorcall", nullptr, -1, meth
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit_efq_tensorcall(void) { return PyModule_Create(&module); }
+// built_for: the torch and Python that it was compiled against, which the binding compares before the first call
+PyMODINIT_FUNC PyInit_efq_tensorcall(void)
+{
+    PyObject* const m = PyModule_Create(&module);
+    if (m != nullptr && PyModule_AddStringConstant(m, "built_for", EFQ_BUILT_FOR) != 0) {
+        Py_DECREF(m);
+        return nullptr;
+    }
+    return m;
+}
