@@ -61,39 +61,47 @@ def _start_tensorcall(out: str):
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
+    """Builds what is not up to date.  The library stands, and C programs have it, also where an extension beside it fails to build."""
     if not force and not _stale():
         return LIB
-    objs = []
     os.makedirs(os.path.join(_HERE, "build"), exist_ok=True)
-    procs = []
-    tensorcall_tmp = TENSORCALL + f".tmp{os.getpid()}"
-    tensorcall = _start_tensorcall(tensorcall_tmp)
-    for src in sources():
-        obj = os.path.join(_HERE, "build", os.path.basename(src)[:-3] + ".o")
-        cmd = [NVCC, *FLAGS, "-c", src, "-o", obj] + (["-Xptxas", "-v"] if verbose else [])
-        procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
-        objs.append(obj)
-    for src, p in procs:
+    tmp = {out: out + f".tmp{os.getpid()}" for out in (LIB, FASTCALL, TENSORCALL)}
+    running = []
+
+    def done(what, p):
         out, _ = p.communicate()
         if verbose or p.returncode != 0:
             sys.stderr.write(out)
         if p.returncode != 0:
-            raise RuntimeError(f"nvcc failed on {src}")
-    tmp = LIB + f".tmp{os.getpid()}"
-    subprocess.run([NVCC, "-shared", "-o", tmp, *objs, "-lcuda", "-cudart", "static"], check=True)
-    os.replace(tmp, LIB)
-    tmp = FASTCALL + f".tmp{os.getpid()}"
-    subprocess.run([os.environ.get("CC", "gcc"), "-O2", "-Wall", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"],
-                    "-I", os.path.join(ROOT, "include"), FASTCALL_SRC, "-o", tmp], check=True)
-    os.replace(tmp, FASTCALL)
-    out, _ = tensorcall.communicate()
-    if verbose or tensorcall.returncode != 0:
-        sys.stderr.write(out)
-    if tensorcall.returncode != 0:
-        raise RuntimeError(f"g++ failed on {TENSORCALL_SRC}")
-    os.replace(tensorcall_tmp, TENSORCALL)
-    with open(BUILT_FOR, "w") as f:
-        f.write(target())
+            raise RuntimeError(f"{p.args[0]} failed on {what}")
+
+    try:
+        running.append(_start_tensorcall(tmp[TENSORCALL]))
+        objs, compiling = [], []
+        for src in sources():
+            objs.append(os.path.join(_HERE, "build", os.path.basename(src)[:-3] + ".o"))
+            cmd = [NVCC, *FLAGS, "-c", src, "-o", objs[-1]] + (["-Xptxas", "-v"] if verbose else [])
+            compiling.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
+            running.append(compiling[-1][1])
+        for src, p in compiling:
+            done(src, p)
+        subprocess.run([NVCC, "-shared", "-o", tmp[LIB], *objs, "-lcuda", "-cudart", "static"], check=True)
+        os.replace(tmp[LIB], LIB)
+        subprocess.run([os.environ.get("CC", "gcc"), "-O2", "-Wall", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"],
+                        "-I", os.path.join(ROOT, "include"), FASTCALL_SRC, "-o", tmp[FASTCALL]], check=True)
+        os.replace(tmp[FASTCALL], FASTCALL)
+        done(TENSORCALL_SRC, running[0])
+        os.replace(tmp[TENSORCALL], TENSORCALL)
+        with open(BUILT_FOR, "w") as f:
+            f.write(target())
+    finally:                # of a build that has failed: neither compilers that go on nor files that they were writing
+        for p in running:
+            if p.poll() is None:
+                p.kill()
+                p.communicate()
+        for path in tmp.values():
+            if os.path.exists(path):
+                os.remove(path)
     return LIB
 
 
