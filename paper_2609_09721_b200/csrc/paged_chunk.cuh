@@ -21,10 +21,7 @@
 
 namespace efq {
 
-// What a query tile costs beside its key tiles, in key tiles.  With 0, 1, 2 and 3: a mixed batch of 16 sequences 290, 281, 276 and 279 us, 300 tokens on
-// 9000 59.6, 58.1, 57.0 and 57.2, 64 on 2000 21.5, 21.4, 21.5 and 22.2.
-constexpr int kChunkItem = 2;
-constexpr int kChunkShift = 7, kChunkKeys = 1 << kChunkShift, kChunkRows = 128;      // keys of a tile, rows of a half
+constexpr int kChunkKeys = 1 << kChunkShift, kChunkRows = 128;      // keys of a tile, rows of a half
 constexpr int kChunkThreads = 384;
 constexpr int kChunkSlots = 5;
 constexpr int kChunkPart = kChunkKeys * 128;                   // bytes of 64 channels of 128 rows

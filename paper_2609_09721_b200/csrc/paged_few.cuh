@@ -16,8 +16,7 @@
 
 namespace efq {
 
-constexpr int kFewItem = 2;                     // what a query tile costs beside its key tiles, in key tiles (1 and 3: up to 2 % more)
-constexpr int kFewShift = 6, kFewKeys = 1 << kFewShift;       // of a stage
+constexpr int kFewKeys = 1 << kFewShift;        // of a stage
 constexpr int kFewWarps = 8;                    // that compute
 constexpr int kFewThreads = (kFewWarps + 1) * 32;
 constexpr int kFewRows = 16;                     // of a product; a query tile has 16 or 32 rows

@@ -18,6 +18,11 @@
 
 namespace efq {
 
+// Keys of a tile (log2), and what a query tile costs beside its key tiles, in key tiles.  Few rows, 1 and 3 instead of 2: up to 2 % more.  Many rows, with 0,
+// 1, 2 and 3: a mixed batch of 16 sequences 290, 281, 276 and 279 us, 300 tokens on 9000 59.6, 58.1, 57.0 and 57.2, 64 on 2000 21.5, 21.4, 21.5 and 22.2.
+constexpr int kFewShift = 6, kFewItem = 2;
+constexpr int kChunkShift = 7, kChunkItem = 2;
+
 // All numbers of units fit 31 bits: a step that might have more is refused (paged_too_many_units()).  The search for a CTA's run stands before its
 // first load, and it is the instructions that cost there, fetched for the first time; 64 bits made three of one.
 

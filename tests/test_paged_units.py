@@ -146,3 +146,89 @@ def test_runs_hold_every_unit_once(lib, seed):
     total = len(want) + item * len({x[:3] for x in want})
     if want:            # shares are equal, of key tiles and what a query tile costs beside them (which may lie with the CTA after its last key tile)
         assert max(sizes.values()) <= -(-total // min(grid, total)) + item
+
+
+# ------------------------------------------------------------ the same with the constants that the kernels have
+SHIPPED = HARNESS + r"""
+extern "C" int64_t shipped_before(int many, int lq, int len, int step, int causal, int n)
+{
+    return many ? before_of<efq::kChunkShift, efq::kChunkItem>(lq, len, step, causal, n) : before_of<efq::kFewShift, efq::kFewItem>(lq, len, step, causal, n);
+}
+extern "C" int64_t shipped_segments(int many, const int32_t* cu, const int32_t* lens, int n_seqs, int heads, int step, int causal, int grid, int32_t* out, int64_t most)
+{
+    return many ? all_segments<efq::kChunkShift, efq::kChunkItem>(cu, lens, n_seqs, heads, step, causal, grid, out, most)
+                : all_segments<efq::kFewShift, efq::kFewItem>(cu, lens, n_seqs, heads, step, causal, grid, out, most);
+}
+extern "C" void shipped_constants(int many, int* keys, int* item)
+{
+    *keys = 1 << (many ? efq::kChunkShift : efq::kFewShift);
+    *item = many ? efq::kChunkItem : efq::kFewItem;
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def shipped(tmp_path_factory):
+    d = tmp_path_factory.mktemp("shipped")
+    (d / "units.cpp").write_text(SHIPPED)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-I", build.CSRC, str(d / "units.cpp"), "-o", str(d / "shipped.so")], check=True)
+    so = ctypes.CDLL(str(d / "shipped.so"))
+    so.shipped_before.restype = so.shipped_segments.restype = ctypes.c_int64
+    so.shipped_segments.argtypes = [ctypes.c_int] + [ctypes.POINTER(ctypes.c_int32)] * 2 + [ctypes.c_int] * 5 + [ctypes.POINTER(ctypes.c_int32), ctypes.c_int64]
+    return so
+
+
+def _constants(so, many):
+    keys, item = ctypes.c_int(), ctypes.c_int()
+    so.shipped_constants(many, ctypes.byref(keys), ctypes.byref(item))
+    return keys.value, item.value
+
+
+def _steps(many):
+    """New tokens of a query tile for every number of query heads on a KV head."""
+    return sorted({128 // g * 2 for g in range(1, 129)} if many else {rows // g for rows in (16, 32) for g in range(1, 33) if rows >= g})
+
+
+@pytest.mark.parametrize("many", [0, 1])
+def test_units_of_the_kernels_in_closed_form(shipped, many):
+    keys, item = _constants(shipped, many)
+    rng = random.Random(2)
+    for step in _steps(many):
+        for _ in range(60):
+            lq, len_ = rng.choice([1, rng.randint(1, 40), rng.randint(1, 900)]), rng.choice([0, 1, rng.randint(0, 900), rng.randint(0, 9000)])
+            causal = rng.randint(0, 1)
+            want = [n + item for n in _units(lq, len_, step, keys, causal)]
+            for n in {0, 1, len(want) // 2, len(want)} - ({1} if not want else set()):
+                assert shipped.shipped_before(many, lq, len_, step, causal, n) == sum(want[:n]), (lq, len_, step, causal, n)
+
+
+@pytest.mark.parametrize("many", [0, 1])
+@pytest.mark.parametrize("seed", range(40))
+def test_runs_of_the_kernels_hold_every_unit_once(shipped, many, seed):
+    keys, item = _constants(shipped, many)
+    rng = random.Random(1000 + seed)
+    n, heads, grid, step, causal = rng.choice([1, 2, 5, 40, 300]), rng.choice([1, 2, 8]), rng.choice([1, 3, 148]), rng.choice(_steps(many)), rng.randint(0, 1)
+    lens_q = [rng.choice([0, 1, 1, rng.randint(1, 9), rng.randint(1, 300)]) for _ in range(n)]
+    lens_k = [rng.choice([0, 1, rng.randint(1, 200), rng.randint(1, 4000)]) for _ in range(n)]
+    cu = [sum(lens_q[:i]) for i in range(n + 1)]
+    want = [(s, h, cu[s] + t * step, j, u) for s in range(n) for h in range(heads)
+            for t, u in enumerate(_units(lens_q[s], lens_k[s], step, keys, causal)) for j in range(u)]
+    out = (ctypes.c_int32 * (10 * (len(want) + 1)))()
+    got = shipped.shipped_segments(many, (ctypes.c_int32 * (n + 1))(*cu), (ctypes.c_int32 * n)(*lens_k), n, heads, step, causal, grid, out, len(want) + 1)
+    assert got >= 0, got
+    rows = [tuple(out[10 * i:10 * i + 10]) for i in range(got)]
+    assert [(s, h, t0, j, u) for _, _, s, h, t0, _, _, j0, j1, u in rows for j in range(j0, j1)] == want
+    sizes, begun, parts = {}, {}, {}
+    for c, begins, s, h, t0, tokens, base, j0, j1, u in rows:
+        sizes[c] = sizes.get(c, 0) + j1 - j0 + (item if j1 == u else 0)
+        if j0 == 0:
+            begun[s, h, t0] = c
+        if (j0, j1) != (0, u):                                   # a part: two places a CTA, one for a tile that it begins
+            parts.setdefault((c, j0 == 0), []).append((s, h, t0))
+        assert begun[s, h, t0] == begins, (c, s, h, t0, j0)
+        first = t0 - cu[s]
+        assert tokens == min(step, lens_q[s] - first) and base == lens_k[s] - lens_q[s] + first
+    assert all(len(x) == 1 for x in parts.values())
+    total = len(want) + item * len({x[:3] for x in want})
+    if want:
+        assert max(sizes.values()) <= -(-total // min(grid, total)) + item
