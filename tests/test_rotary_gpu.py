@@ -412,3 +412,57 @@ def test_gradients_on_a_side_stream_and_in_a_graph():
     w.copy_(w.flip(2))
     graph.replay()
     assert torch.equal(dq, binding.efq_rotary(w, None, pos, r, inverse=True)[0])
+
+
+@pytest.mark.parametrize("lens,Hq,Hkv,page", [([(1, 1)], 1, 1, 16), ([(1, 1 + 31 * i) for i in range(70)], 32, 8, 16), ([(300, 300)], 4, 4, 64), ([(129, 1000), (0, 7), (5, 5)], 5, 1, 128),
+                                              ([(700, 5000)], 28, 4, 256)])
+@pytest.mark.parametrize("sections,interleaved", [((64,), False), ((22, 21, 21), True), ((20, 12), False), (None, False)])
+def test_append_of_fp16(lens, Hq, Hkv, page, sections, interleaved):
+    """Values up to where the turned ones almost end the type's range, small ones where it has few bits, and a step without a rotation."""
+    p = Paged(lens, Hq, Hkv, page, torch.float16, seed=35, tail=2, token_major=len(lens) > 1)
+    n = int(p.cu[-1])
+    g = torch.Generator(device="cuda").manual_seed(36)
+    sizes = 2.0 ** torch.randint(-20, 13, (p.total, 1, 1), generator=g, device="cuda")           # a size a token: both channels of a pair have it
+    k, v = ((torch.randn(p.total, Hkv, D, generator=g, device="cuda") * sizes).half() for _ in range(2))
+    r = None if sections is None else _rotary(sections, interleaved, False)
+    index = torch.cat([torch.arange(m - a, m) for a, m in lens] + [torch.zeros(2, dtype=torch.long)]).cuda()
+    pos = None if sections is None else torch.stack([index // (3 ** a) for a in range(len(sections))]).int()
+    turned = (lambda x: x.double()) if r is None else lambda x: rotate(x.transpose(0, 1), pos, r.inv_freq, sections, interleaved).transpose(0, 1)  # noqa: E731
+    slack = (lambda x: torch.zeros_like(x, dtype=torch.float64)) if r is None else lambda x: rotate_slack(x, torch.float16, sections, interleaved)  # noqa: E731
+    assert float(k.abs().max()) * 2 ** 0.5 < 65504
+    want_k, want_v = p.d_k_cache.clone(), p.d_v_cache.clone()
+    place = [(int(p.table[s, i // page]), i % page) for s, (a, m) in enumerate(lens) for i in range(m - a, m)]
+    pages, slots = (torch.tensor([x[j] for x in place], device="cuda") for j in (0, 1))
+    q_out = torch.full((p.total, Hq, D), 7.0, dtype=torch.float16, device="cuda")
+    binding.efq_paged_append(k, v, p.d_k_cache, p.d_v_cache, *p.tables, r, pos, p.d_q, q_out)
+    assert (q_out[n:] == 7.0).all()
+    _near(q_out[:n], turned(p.d_q)[:n], slack(p.d_q)[:n])
+    _near(p.d_k_cache[pages, :, slots], turned(k)[:n], slack(k)[:n])
+    want_k[pages, :, slots], want_v[pages, :, slots] = p.d_k_cache[pages, :, slots], v[:n]
+    same = lambda a, b: torch.equal(a.contiguous().view(torch.int16), b.contiguous().view(torch.int16))  # noqa: E731
+    assert same(p.d_k_cache, want_k) and same(p.d_v_cache, want_v)
+
+
+def test_a_step_of_a_model_in_fp16():
+    """Append and attention of one step, against the whole in 64 bits."""
+    Hq, Hkv, page, n, total = 8, 2, 32, 40, 300
+    p = Paged([(n, total)], Hq, Hkv, page, torch.float16, seed=37, hot=0)
+    r = _rotary((64,), False, False)
+    k, v = p.k[0].cuda(), p.v[0].cuda()
+    cu = torch.tensor([0, total], dtype=torch.int32, device="cuda")
+    binding.efq_paged_append(k, v, p.d_k_cache, p.d_v_cache, p.d_table, cu, p.d_seq_lens, r)      # the prompt, its last tokens among it
+    q = binding.efq_paged_append(k[-n:], v[-n:], p.d_k_cache, p.d_v_cache, *p.tables, r, None, p.d_q)
+    o = binding.efq_paged_attention_fwd(q, p.d_k_cache, p.d_v_cache, *p.tables, n)
+    pos = torch.arange(total, device="cuda", dtype=torch.int32)[None]
+    Q = rotate(p.d_q.transpose(0, 1), pos[:, -n:], r.inv_freq, (64,), False)
+    K = rotate(k.transpose(0, 1), pos, r.inv_freq, (64,), False)
+    seen = torch.ones(n, total, dtype=torch.bool, device="cuda").tril(total - n)
+    u = 2.0 ** -11
+    for h in range(Hq):
+        s = Q[h] @ K[h // 4].T / math.sqrt(D)
+        # rotated q and k are rounded: u of each factor of every product, 2 u and u^2 of the sum of sizes
+        ds = (Q[h].abs() @ K[h // 4].abs().T / math.sqrt(D)).amax(1, keepdim=True) * (2.1 * u)
+        w = torch.softmax(s.masked_fill(~seen, -math.inf), dim=1)
+        V = v[:, h // 4].double()
+        tol = (torch.expm1(2 * ds) + 1.1 * u) * (w @ V.abs()) + u * (w @ V).abs() + 2.0 ** -25
+        assert float(((o[:, h].double() - w @ V).abs() - tol).max()) <= 0.0
